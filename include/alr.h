@@ -355,6 +355,137 @@ alr_status alr_ira_assemble(alr_ctx* ctx, int32_t n_primary, int32_t block,
 alr_status alr_slot_weights(alr_ctx* ctx, int32_t n, int32_t block, const int32_t* tokens,
                             int32_t eos_id, float gamma, float* weight_out, alr_stream stream);
 
+/* Limits of a draw, per row; DEVICE arrays, each may be NULL (off for every row). */
+typedef struct {
+  const float* temperature; /* NULL: 1.  <= 0 or nan: greedy                       */
+  const int32_t* top_k;     /* <= 0 or >= vocab: off                               */
+  const float* top_p;       /* >= 1 or nan: off                                    */
+  const float* min_p;       /* <= 0 or nan: off; above 1: as 1                     */
+} alr_sampling;
+
+/* Largest vocabulary that tokens are drawn from. */
+#define ALR_SAMPLE_MAX_VOCAB 524288
+
+/* One token per row of logits, drawn by a given uniform number.
+ * Tokens are ranked by decreasing logit, equal logits by increasing id, and
+ * weigh w_v = exp((z_v - max z) / temperature).  Kept is the shortest of these
+ * prefixes of the ranking: the first top_k; the smallest one that holds at least
+ * top_p of the weight of the first top_k; the tokens with w_v >= min_p (min_p
+ * times the largest probability).  The first token is always kept.  The token
+ * drawn is the first, in the order of the ids, whose cumulative kept weight
+ * exceeds uniform times the whole kept weight.  Greedy rows take the lowest id
+ * at the maximum.  Logits that are nan count as -inf.  A row without a logit above
+ * -inf gives token -1, log-prob -inf; a row with logits of +inf is greedy.
+ *   n, vocab    rows, and values per row (1 .. ALR_SAMPLE_MAX_VOCAB).
+ *   logits      DEVICE, dtype ALR_F32 or ALR_BF16 (independent of the context's), row r at
+ *               r * row_stride elements; row_stride >= vocab, any alignment.
+ *   sampling    HOST struct of DEVICE arrays [n], or NULL: no limits.
+ *   uniform     DEVICE fp32 [n], in [0, 1) (values outside are clamped into it).
+ *   tokens_out  DEVICE int32 [n].
+ *   logp_out    DEVICE fp32 [n] or NULL: log of the probability with which the
+ *               token was drawn, its share of the kept weight (0 for a greedy row).
+ * Weights are formed in 64 bits and rounded to 2^-43 or less of the largest, so
+ * their sums are exact: what a row gives depends on that row alone.  n = 0 is a
+ * no-op. */
+alr_status alr_sample(alr_ctx* ctx, int32_t n, int32_t vocab, const void* logits, int32_t dtype,
+                      int64_t row_stride, const alr_sampling* sampling, const float* uniform,
+                      int32_t* tokens_out, float* logp_out, alr_stream stream);
+
+/* Rollout under a sampled policy: alr_rollout / alr_rollout_topk with the fed
+ * tokens drawn as alr_sample draws them, from each slot's fp32 logits (the paper's greedy
+ * rollout is temperature 0).  Arguments and checks as in alr_rollout_topk, and:
+ *   sampling    HOST struct of DEVICE arrays [n_anchor] in the caller's anchor
+ *               order, each holding for all slots of its anchor, or NULL.
+ *   uniform     DEVICE fp32 [n_anchor, block].
+ *   tokens_out  DEVICE int32 [n_anchor, block]: the token drawn at every slot
+ *               (where forced[i,s] >= 0 that is fed to slot s+1 instead).
+ *   token_logp_out  DEVICE fp32 [n_anchor, block] or NULL: alr_sample's logp_out.
+ *   top_ids_out, top_logp_out, tail_out  as in alr_rollout_topk (the policy's own
+ *               labels, without temperature or limits), or all NULL.
+ *   logprobs_out, feats_out  as in alr_rollout_topk, each may be NULL.
+ * Tokens are the same whatever other outputs are asked for.  Rollout graphs
+ * (alr_set_rollout_graphs) replay with the values that the arrays hold then. */
+alr_status alr_rollout_sampled(alr_ctx* ctx, int32_t n_anchor, const int32_t* anchor_seq,
+                               const int32_t* anchor_pos, int32_t block,
+                               const alr_sampling* sampling, const float* uniform,
+                               const int32_t* forced, int32_t* tokens_out, float* token_logp_out,
+                               int32_t* top_ids_out, float* top_logp_out, float* tail_out,
+                               float* logprobs_out, float* feats_out, alr_stream stream);
+
+/* The distillation loss on top-8 + tail labels, and its gradient (Sec. 3.1, Eq. 1;
+ * App. A, the loss row of the training table).  Row r holds a drafter's logits
+ * z; its label is one slot of alr_rollout_topk, alr_corpus_labels or
+ * alr_ira_assemble.  With q = softmax(z), pi_j = exp(top_logp[r,j]), S the listed
+ * tokens and P = sum_j pi_j + tail[r]:
+ *   row_loss = - sum_j pi_j log q_(id_j) - tail log(sum of q outside S)
+ *   loss     = scale * sum_r weight_r row_loss_r / W,  W = sum_r weight_r
+ * (terms of zero probability are 0; loss is 0 where W is 0).  The gradient of loss,
+ * times grad_out, by z_v is grad_out scale weight_r / W times
+ *   P q_v - sum_{j: id_j = v} pi_j                     for v in S
+ *   P q_v - tail q_v / (sum of q outside S)            otherwise.
+ *   n, vocab, logits, dtype, row_stride  as in alr_sample (any vocab >= 1).
+ *   top_ids, top_logp  DEVICE [n, ALR_TOPK]; an id outside [0, vocab) (-1 pads a
+ *               label, a cut vocabulary may lack a token) is passed over with its
+ *               probability.  An id listed twice adds up.
+ *   tail        DEVICE fp32 [n].
+ *   weight      DEVICE fp32 [n] (alr_slot_weights, an erase gate), or NULL: 1.
+ *               A row of weight 0 is not read: its row_loss and gradient are 0.
+ *   scale       factor of the loss (the paper's KD scale).
+ *   grad_out    DEVICE fp32 [1]: gradient that arrives at the loss; NULL: 1.
+ *   loss_out    DEVICE fp32 [2]: loss and W.
+ *   row_loss_out  DEVICE fp32 [n].
+ *   dlogits_out DEVICE, rows of the logits' dtype at dlogits_stride elements, or
+ *               NULL: no gradient.  May be the logits themselves (same stride), else
+ *               must not overlap them.
+ * Sums are fp32 within a row, 64-bit over the rows, in an order that does not change from
+ * call to call.  n = 0 gives loss 0 and W 0. */
+alr_status alr_distill_loss(alr_ctx* ctx, int32_t n, int32_t vocab, const void* logits,
+                            int32_t dtype, int64_t row_stride, const int32_t* top_ids,
+                            const float* top_logp, const float* tail, const float* weight,
+                            float scale, const float* grad_out, float* loss_out,
+                            float* row_loss_out, void* dlogits_out, int64_t dlogits_stride,
+                            alr_stream stream);
+
+/* RMSNorm of every query and key head, and the position rotation, in one pass:
+ * each head x of head_dim values becomes RoPE_pos(x g / sqrt(mean(x^2) + eps)),
+ * with the context's head_dim, dtype, rms_eps, rope_base and mrope_sections.
+ *   n           rows (tokens); q_heads, k_heads >= 0 heads of each (not both 0).
+ *   positions   DEVICE int32 [n, 3]: (t, h, w) position of every row (only t without
+ *               mrope_sections), or NULL: the row's index (then n <= max_pos).  A row
+ *               with a position outside [0, max_pos) becomes nan.
+ *   q, k        DEVICE, row r at r * stride elements, its heads next to each other
+ *               (so q and k may be column ranges of one projection's output).
+ *   q_gain, k_gain  DEVICE [head_dim].
+ *   q_out, k_out  DEVICE rows as q and k; may be q and k themselves.
+ * Arguments of a kind without heads are not looked at.  n = 0 is a no-op. */
+alr_status alr_qk_norm_rope(alr_ctx* ctx, int32_t n, int32_t q_heads, int32_t k_heads,
+                            const int32_t* positions, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const void* q_gain,
+                            const void* k_gain, void* q_out, int64_t q_out_stride, void* k_out,
+                            int64_t k_out_stride, alr_stream stream);
+
+/* Gradients of alr_qk_norm_rope: from its inputs and the gradients of its outputs
+ * (dq_out, dk_out) those of q and k (dq, dk; may be dq_out and dk_out themselves) and of the gains,
+ * summed over rows and heads in fp32 in a fixed order (dq_gain, dk_gain: DEVICE fp32
+ * [head_dim]; 0 for n = 0).  Uses the context's workspace. */
+alr_status alr_qk_norm_rope_backward(alr_ctx* ctx, int32_t n, int32_t q_heads, int32_t k_heads,
+                                     const int32_t* positions, const void* q, int64_t q_stride,
+                                     const void* k, int64_t k_stride, const void* q_gain,
+                                     const void* k_gain, const void* dq_out, int64_t dq_out_stride,
+                                     const void* dk_out, int64_t dk_out_stride, void* dq,
+                                     int64_t dq_stride, void* dk, int64_t dk_stride,
+                                     float* dq_gain, float* dk_gain, alr_stream stream);
+
+/* Per-head norms of queries and keys in the model itself (the Qwen3 family, the
+ * paper's targets): from the next prefill on, every layer passes q and k through
+ * alr_qk_norm_rope instead of the rotation alone.  In ALR_BF16 the projections' q and k are
+ * rounded to bf16 before the norm too.
+ *   q_gain, k_gain  HOST arrays of n_layers DEVICE pointers to head_dim values of
+ *               the weight dtype, copied on `stream`; both NULL: off (the default).
+ * Drops the prefill and the rollout graphs; not allowed while `stream` is captured. */
+alr_status alr_set_qk_norm(alr_ctx* ctx, const void* const* q_gain, const void* const* k_gain,
+                           alr_stream stream);
+
 /* Message of the last failing call on ctx ("" if none); ctx may be NULL, then
  * the message of the last failing alr_create in this thread is returned. */
 const char* alr_last_error(const alr_ctx* ctx);

@@ -125,6 +125,14 @@ def rmsnorm(x: np.ndarray, g: np.ndarray, eps: float) -> np.ndarray:
     return x / np.sqrt(ms + eps) * g
 
 
+def head_norm(P: "Params", name: str, layer: int, x: np.ndarray, eps: float, rnd) -> np.ndarray:
+    """x[T, heads, hd] normed per head by the gains ``name`` of the layer, if the weights have them
+    (the q/k norms of the Qwen3 family); the projection's output is then rounded first."""
+    if name not in P.w["layers"][layer]:
+        return x
+    return rmsnorm(rnd(x), P.get(name, layer), eps)
+
+
 def silu(x: np.ndarray) -> np.ndarray:
     return x / (1.0 + np.exp(-x))
 
@@ -239,8 +247,8 @@ def decoder_forward(P: Params, shape, x0: np.ndarray, positions: np.ndarray,
     outs: List[np.ndarray] = []
     for layer in range(shape.n_layers):
         n1 = rnd(rmsnorm(h, P.get("attn_norm", layer), eps))
-        q = (n1 @ P.get("wq", layer).T).reshape(T, H, hd)
-        k = (n1 @ P.get("wk", layer).T).reshape(T, G, hd)
+        q = head_norm(P, "q_norm", layer, (n1 @ P.get("wq", layer).T).reshape(T, H, hd), eps, rnd)
+        k = head_norm(P, "k_norm", layer, (n1 @ P.get("wk", layer).T).reshape(T, G, hd), eps, rnd)
         v = (n1 @ P.get("wv", layer).T).reshape(T, G, hd)
         q = rnd(rope(q, positions, shape.rope_base, _sections(shape)))
         k = rnd(rope(k, positions, shape.rope_base, _sections(shape)))
@@ -278,11 +286,12 @@ def decoder_layer_at(P: Params, shape, layer: int, x: np.ndarray, positions: np.
     h_all = x[:T].astype(dt)
     pos = np.asarray(positions)[:T]
     n1 = rnd(rmsnorm(h_all, P.get("attn_norm", layer), eps))
-    k = rnd(rope((n1 @ P.get("wk", layer).T).reshape(T, G, hd), pos, shape.rope_base,
-                 _sections(shape)))
+    k = head_norm(P, "k_norm", layer, (n1 @ P.get("wk", layer).T).reshape(T, G, hd), eps, rnd)
+    k = rnd(rope(k, pos, shape.rope_base, _sections(shape)))
     v = rnd((n1 @ P.get("wv", layer).T).reshape(T, G, hd))
-    q = rnd(rope((n1[rows] @ P.get("wq", layer).T).reshape(len(rows), H, hd), pos[rows],
-                 shape.rope_base, _sections(shape)))
+    q = head_norm(P, "q_norm", layer, (n1[rows] @ P.get("wq", layer).T).reshape(len(rows), H, hd),
+                  eps, rnd)
+    q = rnd(rope(q, pos[rows], shape.rope_base, _sections(shape)))
     o = rnd(causal_gqa_attention(q, k, v, rp, q_pos=rows).reshape(len(rows), H * hd))
     h = h_all[rows] + o @ P.get("wo", layer).T
     n2 = rnd(rmsnorm(h, P.get("ffn_norm", layer), eps))
@@ -454,9 +463,11 @@ def rollout_kv_shared(P: Params, shape, tokens: np.ndarray, anchor_seq, anchor_p
         Ks, Vs, outs = [], [], []
         for layer in range(L):
             n1 = rmsnorm(h, P.get("attn_norm", layer), eps)
-            q = rope((n1 @ P.get("wq", layer).T).reshape(T, H, hd), pos, shape.rope_base,
+            q = (n1 @ P.get("wq", layer).T).reshape(T, H, hd)
+            q = rope(head_norm(P, "q_norm", layer, q, eps, _ident), pos, shape.rope_base,
                      _sections(shape))
-            k = rope((n1 @ P.get("wk", layer).T).reshape(T, G, hd), pos, shape.rope_base,
+            k = (n1 @ P.get("wk", layer).T).reshape(T, G, hd)
+            k = rope(head_norm(P, "k_norm", layer, k, eps, _ident), pos, shape.rope_base,
                      _sections(shape))
             v = (n1 @ P.get("wv", layer).T).reshape(T, G, hd)
             Ks.append(k)
@@ -497,9 +508,11 @@ def rollout_kv_shared(P: Params, shape, tokens: np.ndarray, anchor_seq, anchor_p
         outs = []
         for layer in range(L):
             n1 = rmsnorm(h, P.get("attn_norm", layer), eps)
-            q = rope((n1 @ P.get("wq", layer).T).reshape(n, H, hd), pos, shape.rope_base,
+            q = (n1 @ P.get("wq", layer).T).reshape(n, H, hd)
+            q = rope(head_norm(P, "q_norm", layer, q, eps, _ident), pos, shape.rope_base,
                      _sections(shape))
-            k = rope((n1 @ P.get("wk", layer).T).reshape(n, G, hd), pos, shape.rope_base,
+            k = (n1 @ P.get("wk", layer).T).reshape(n, G, hd)
+            k = rope(head_norm(P, "k_norm", layer, k, eps, _ident), pos, shape.rope_base,
                      _sections(shape))
             v = (n1 @ P.get("wv", layer).T).reshape(n, G, hd)
             o = np.zeros((n, H, hd), P.dt)

@@ -27,7 +27,8 @@ EXPORTS = ("alr_workspace_bytes", "alr_check_config", "alr_check_rollout", "alr_
            "alr_rollout_topk_noalloc",
            "alr_corpus_labels", "alr_ira_assemble", "alr_slot_weights", "alr_last_error", "alr_status_string", "alr_destroy",
            "alr_debug_gemm", "alr_debug_decode_plan", "alr_debug_gemm_plan", "alr_profile_start", "alr_profile_stop",
-           "alr_set_rollout_graphs")
+           "alr_set_rollout_graphs", "alr_sample", "alr_rollout_sampled", "alr_distill_loss",
+           "alr_qk_norm_rope", "alr_qk_norm_rope_backward", "alr_set_qk_norm")
 ALR_TOPK = 8
 
 
@@ -55,6 +56,11 @@ class AlrWeights(ctypes.Structure):
                 ("lm_head", ctypes.c_void_p), ("attn_norm", _PP), ("wq", _PP), ("wk", _PP),
                 ("wv", _PP), ("wo", _PP), ("ffn_norm", _PP), ("w_gate", _PP), ("w_up", _PP),
                 ("w_down", _PP)]
+
+
+class AlrSampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
+                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
 
 
 class AlrError(RuntimeError):
@@ -125,6 +131,23 @@ def load_library() -> ctypes.CDLL:
     lib.alr_profile_stop.restype = ctypes.c_int
     lib.alr_set_rollout_graphs.argtypes = [vp, i32]
     lib.alr_set_rollout_graphs.restype = ctypes.c_int
+    i64, f32, smp = ctypes.c_int64, ctypes.c_float, ctypes.POINTER(AlrSampling)
+    lib.alr_sample.argtypes = [vp, i32, i32, vp, i32, i64, smp, vp, vp, vp, vp]
+    lib.alr_sample.restype = ctypes.c_int
+    lib.alr_rollout_sampled.argtypes = [vp, i32, i32p, i32p, i32, smp, vp, vp, vp, vp, vp, vp, vp,
+                                        vp, vp, vp]
+    lib.alr_rollout_sampled.restype = ctypes.c_int
+    lib.alr_distill_loss.argtypes = [vp, i32, i32, vp, i32, i64, vp, vp, vp, vp, f32, vp, vp, vp,
+                                     vp, i64, vp]
+    lib.alr_distill_loss.restype = ctypes.c_int
+    lib.alr_qk_norm_rope.argtypes = [vp, i32, i32, i32, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp,
+                                     i64, vp]
+    lib.alr_qk_norm_rope.restype = ctypes.c_int
+    lib.alr_qk_norm_rope_backward.argtypes = [vp, i32, i32, i32, vp, vp, i64, vp, i64, vp, vp, vp,
+                                              i64, vp, i64, vp, i64, vp, i64, vp, vp, vp]
+    lib.alr_qk_norm_rope_backward.restype = ctypes.c_int
+    lib.alr_set_qk_norm.argtypes = [vp, _PP, _PP, vp]
+    lib.alr_set_qk_norm.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -193,7 +216,8 @@ class Engine:
     """One library context: weights repacked into a caller-owned workspace.
 
     ``weights`` is the generator's dict (numpy float32 or uint16 bf16 bits);
-    they are uploaded, repacked by the library and released again.
+    they are uploaded, repacked by the library and released again.  Layers with
+    ``q_norm`` and ``k_norm`` gains [head_dim] turn the per-head q/k norms on.
     """
 
     def __init__(self, shape, weights: Dict, max_pos: int, limits: AlrLimits, device="cuda",
@@ -235,6 +259,9 @@ class Engine:
         if st != 0:
             raise AlrError(st, self.lib.alr_last_error(None).decode())
         self.ctx = ctx
+        if any("q_norm" in ld or "k_norm" in ld for ld in weights["layers"]):
+            self.set_qk_norm([ld["q_norm"] for ld in weights["layers"]],
+                             [ld["k_norm"] for ld in weights["layers"]])
         del dev_w, keep
 
     def _sp(self):
@@ -417,6 +444,214 @@ class Engine:
         if st != 0:
             self._err(st)
         return w
+
+
+    # ------------------------------------------- operators on the caller's tensors
+    def _tensor(self, name, t, shape, dtypes, strided=False):
+        """Checks a device tensor argument (the library sees only its address): on this
+        context's device, of the shape and a dtype asked for, contiguous, or, `strided`, rows of
+        contiguous values at any row stride."""
+        if t.device != self.workspace.device:
+            raise ValueError(f"{name}: on {t.device}, the context is on {self.workspace.device}")
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if t.dtype not in dtypes:
+            raise ValueError(f"{name}: dtype {t.dtype}, expected {' or '.join(map(str, dtypes))}")
+        if strided:
+            if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+                raise ValueError(f"{name}: rows must be contiguous and must not overlap")
+        elif not t.is_contiguous():
+            raise ValueError(f"{name}: must be contiguous")
+        return t.data_ptr()
+
+    @staticmethod
+    def _row_stride(t):
+        return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+    def _dtype_code(self, t):
+        return ALR_BF16 if t.dtype == self.torch.bfloat16 else ALR_F32
+
+    def _sampling(self, n, temperature, top_k, top_p, min_p):
+        torch = self.torch
+        if temperature is None and top_k is None and top_p is None and min_p is None:
+            return None
+        sp = AlrSampling()
+        for name, t, dt in (("temperature", temperature, torch.float32),
+                            ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                            ("min_p", min_p, torch.float32)):
+            if t is not None:
+                setattr(sp, name, self._tensor(name, t, (n,), (dt,)))
+        return ctypes.byref(sp)
+
+    def sample(self, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None,
+               out=None):
+        """One token per row of logits [n, vocab] (bf16 or fp32, any row stride) by the uniform
+        numbers [n]; limits are fp32 (top_k: int32) tensors [n] or None.  -> (tokens int32 [n],
+        log-probs fp32 [n] of the draws), into ``out`` if given (its second entry may be None)."""
+        torch = self.torch
+        n, V = logits.shape
+        lp = self._tensor("logits", logits, (n, V), (torch.bfloat16, torch.float32), strided=True)
+        sp = self._sampling(n, temperature, top_k, top_p, min_p)
+        up = self._tensor("uniform", uniform, (n,), (torch.float32,))
+        if out is None:
+            out = (torch.empty(n, dtype=torch.int32, device=self.device),
+                   torch.empty(n, dtype=torch.float32, device=self.device))
+        tok, logp = out
+        st = self.lib.alr_sample(
+            self.ctx, n, V, lp, self._dtype_code(logits), self._row_stride(logits), sp, up,
+            self._tensor("tokens", tok, (n,), (torch.int32,)),
+            None if logp is None else self._tensor("logp", logp, (n,), (torch.float32,)),
+            self._sp())
+        if st != 0:
+            self._err(st)
+        return tok, logp
+
+    def rollout_sampled(self, anchor_seq, anchor_pos, block: int, uniform, temperature=None,
+                        top_k=None, top_p=None, min_p=None, forced=None, want_topk: bool = True,
+                        want_logprobs: bool = False, want_feats: bool = True, out=None):
+        """Rollout whose fed tokens are drawn from the uniform numbers [n_anchor, block]; limits are
+        tensors [n_anchor] or None.  -> (tokens, token log-probs, top_ids, top_logp, tail, logprobs,
+        feats), the forms not wanted None."""
+        torch = self.torch
+        a_s = np.ascontiguousarray(anchor_seq, dtype=np.int32)
+        a_p = np.ascontiguousarray(anchor_pos, dtype=np.int32)
+        n = len(a_s)
+        f32 = dict(dtype=torch.float32, device=self.device)
+        if out is None:
+            ti, tl, tt = self.alloc_topk(n, block) if want_topk else (None, None, None)
+            out = (torch.empty((n, block), dtype=torch.int32, device=self.device),
+                   torch.empty((n, block), **f32), ti, tl, tt,
+                   torch.empty((n, block, self.shape.vocab), **f32) if want_logprobs else None,
+                   torch.empty((n, block, self.shape.n_feat, self.shape.d_model), **f32)
+                   if want_feats and self.shape.n_feat > 0 else None)
+        ptr = (lambda t: None if t is None else t.data_ptr())
+        st = self.lib.alr_rollout_sampled(
+            self.ctx, n, _i32p(a_s), _i32p(a_p), block,
+            self._sampling(n, temperature, top_k, top_p, min_p),
+            self._tensor("uniform", uniform, (n, block), (torch.float32,)), ptr(forced),
+            *(ptr(t) for t in out), self._sp())
+        if st != 0:
+            self._err(st)
+        return out
+
+    def distill_loss(self, logits, top_ids, top_logp, tail, weight=None, scale: float = 1.0,
+                     grad_out=None, want_grad: bool = True, out=None):
+        """Distillation loss of a drafter's logits [n, vocab] (bf16 or fp32, any row stride) on labels
+        of n slots ([n, 8], or [anchors, block, 8] with n = anchors * block, as the rollouts return
+        them).  grad_out: device fp32 tensor of one value, the gradient of the loss.  -> (fp32 [2]:
+        loss and sum of weights, row losses [n], gradient of the logits or None), into ``out`` if given;
+        its gradient may be the logits tensor itself."""
+        torch = self.torch
+        n, V = logits.shape
+        f32 = (torch.float32,)
+        lp = self._tensor("logits", logits, (n, V), (torch.bfloat16, torch.float32), strided=True)
+        label = [self._tensor("top_ids", top_ids.reshape(-1, ALR_TOPK), (n, ALR_TOPK), (torch.int32,)),
+                 self._tensor("top_logp", top_logp.reshape(-1, ALR_TOPK), (n, ALR_TOPK), f32),
+                 self._tensor("tail", tail.reshape(-1), (n,), f32),
+                 None if weight is None else self._tensor("weight", weight.reshape(-1), (n,), f32)]
+        if not all(t is None or t.is_contiguous() for t in (top_ids, top_logp, tail, weight)):
+            raise ValueError("labels and weights must be contiguous")
+        if out is None:
+            out = (torch.empty(2, dtype=torch.float32, device=self.device),
+                   torch.empty(n, dtype=torch.float32, device=self.device),
+                   torch.empty((n, V), dtype=logits.dtype, device=self.device) if want_grad else None)
+        loss, row, dz = out
+        st = self.lib.alr_distill_loss(
+            self.ctx, n, V, lp, self._dtype_code(logits), self._row_stride(logits), *label, scale,
+            None if grad_out is None else self._tensor("grad_out", grad_out.reshape(-1), (1,), f32),
+            self._tensor("loss", loss, (2,), f32), self._tensor("row_loss", row, (n,), f32),
+            None if dz is None else self._tensor("dlogits", dz, (n, V), (logits.dtype,), strided=True),
+            V if dz is None else self._row_stride(dz), self._sp())
+        if st != 0:
+            self._err(st)
+        return out
+
+    def _heads(self, name, t, n):
+        """(heads, address, row stride) of rows of heads, or of None."""
+        torch = self.torch
+        if t is None:
+            return 0, None, 0
+        hd = self.shape.head_dim
+        dt = torch.bfloat16 if self.shape.dtype == "bf16" else torch.float32
+        if t.dim() != 2 or t.shape[1] % hd or t.shape[1] == 0:
+            raise ValueError(f"{name}: shape {tuple(t.shape)} is no rows of {hd}-value heads")
+        return (t.shape[1] // hd, self._tensor(name, t, (n, t.shape[1]), (dt,), strided=True),
+                self._row_stride(t))
+
+    def qk_norm_rope(self, q, k, q_gain, k_gain, positions=None, out=None):
+        """RMSNorm and rotation of every head of q [n, q_heads * head_dim] and k, tensors of the
+        context's dtype (row views of a projection's output do); q or k may be None.  positions: device
+        int32 [n, 3] or None (the row's index).  -> (q_out, k_out), into ``out`` if given (in place:
+        out=(q, k))."""
+        torch = self.torch
+        n = (q if q is not None else k).shape[0]
+        if out is None:
+            out = tuple(None if t is None else torch.empty(t.shape, dtype=t.dtype, device=self.device)
+                        for t in (q, k))
+        (H, qp, qs), (G, kp, ks) = self._heads("q", q, n), self._heads("k", k, n)
+        (Ho, qop, qos), (Go, kop, kos) = self._heads("q_out", out[0], n), self._heads("k_out", out[1], n)
+        if (H, G) != (Ho, Go):
+            raise ValueError("outputs must have the heads of q and k")
+        st = self.lib.alr_qk_norm_rope(
+            self.ctx, n, H, G, self._positions(positions, n), qp, qs, kp, ks,
+            self._gain("q_gain", q_gain, H), self._gain("k_gain", k_gain, G), qop, qos, kop, kos,
+            self._sp())
+        if st != 0:
+            self._err(st)
+        return out
+
+    def qk_norm_rope_backward(self, q, k, q_gain, k_gain, dq_out, dk_out, positions=None, out=None):
+        """Gradients of qk_norm_rope from those of its outputs.  -> (dq, dk, dq_gain, dk_gain), the
+        gains' in fp32 [head_dim], into ``out`` if given (dq and dk may be dq_out and dk_out)."""
+        torch = self.torch
+        n, hd = (q if q is not None else k).shape[0], self.shape.head_dim
+        if out is None:
+            out = tuple(None if t is None else torch.empty(t.shape, dtype=t.dtype, device=self.device)
+                        for t in (q, k))
+            out += tuple(None if t is None else torch.empty(hd, dtype=torch.float32, device=self.device)
+                         for t in (q, k))
+        (H, qp, qs), (G, kp, ks) = self._heads("q", q, n), self._heads("k", k, n)
+        ins = self._heads("dq_out", dq_out, n), self._heads("dk_out", dk_out, n)
+        outs = self._heads("dq", out[0], n), self._heads("dk", out[1], n)
+        if any((a[0], b[0]) != (H, G) for a, b in (ins, outs)):
+            raise ValueError("gradients must have the heads of q and k")
+        gain = [None if t is None else self._tensor(nm, t, (hd,), (torch.float32,))
+                for nm, t in (("dq_gain", out[2]), ("dk_gain", out[3]))]
+        st = self.lib.alr_qk_norm_rope_backward(
+            self.ctx, n, H, G, self._positions(positions, n), qp, qs, kp, ks,
+            self._gain("q_gain", q_gain, H), self._gain("k_gain", k_gain, G), *ins[0][1:], *ins[1][1:],
+            *outs[0][1:], *outs[1][1:], *gain, self._sp())
+        if st != 0:
+            self._err(st)
+        return out
+
+    def _positions(self, positions, n):
+        if positions is None:
+            return None
+        return self._tensor("positions", positions, (n, 3), (self.torch.int32,))
+
+    def _gain(self, name, g, heads):
+        torch = self.torch
+        if heads == 0:
+            return None
+        dt = torch.bfloat16 if self.shape.dtype == "bf16" else torch.float32
+        return self._tensor(name, g, (self.shape.head_dim,), (dt,))
+
+    def set_qk_norm(self, q_gain=None, k_gain=None):
+        """alr_set_qk_norm: per-layer gains [head_dim] (numpy, as the other weights) that turn the
+        model's q/k norms on, or None for both: off.  Prefill anew afterwards."""
+        if q_gain is None and k_gain is None:
+            st = self.lib.alr_set_qk_norm(self.ctx, None, None, self._sp())
+        else:
+            hd, nl = self.shape.head_dim, self.shape.n_layers
+            if any(len(gs) != nl or any(g.shape != (hd,) for g in gs) for gs in (q_gain, k_gain)):
+                raise ValueError(f"q/k norm gains: {nl} layers of {hd} values each")
+            dev = [[self._to_dev(g) for g in gs] for gs in (q_gain, k_gain)]
+            arr = [(ctypes.c_void_p * max(1, nl))(*[t.data_ptr() for t in ts]) for ts in dev]
+            st = self.lib.alr_set_qk_norm(self.ctx, *(ctypes.cast(a, _PP) for a in arr), self._sp())
+            self.stream.synchronize()  # the copies have read the gains
+        if st != 0:
+            self._err(st)
 
 
 PROF_SITES = {"prefill_qkv": 1, "prefill_attn": 2, "prefill_o": 3, "prefill_gu": 4,

@@ -25,7 +25,7 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
 // < sec0 follow axis t, < sec01 axis h, the rest axis w.  Formed once per pass by
 // the embedding kernel, so that no layer's QKV epilogue looks a position up.
 struct RopeRows {
-  f32x2* rope;       // [rows, half]
+  f32x2* rope;       // [rows, half], or null: not formed
   const f32x2* tab;  // [max_pos, half]
   const int* pos;
   int pos_add, half, sec0, sec01;
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void embed_kernel(float* __restrict__ resid,
   const bool use_given = mask != nullptr && mask[r] != 0;
   const T* src = use_given ? given + r * d : E + (long)tok[r] * d;
   float* dst = resid + r * d;
-  for (int i = threadIdx.x; i < rr.half; i += 256) {
+  for (int i = threadIdx.x; rr.rope != nullptr && i < rr.half; i += 256) {
     const int axis = (i < rr.sec0) ? 0 : ((i < rr.sec01) ? 1 : 2);
     rr.rope[r * rr.half + i] = rr.tab[(long)(rr.pos[3 * r + axis] + rr.pos_add) * rr.half + i];
   }

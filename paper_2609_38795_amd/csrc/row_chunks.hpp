@@ -1,0 +1,92 @@
+// Rows of logits as 16-byte chunks, for the kernels that walk a whole vocabulary row per
+// workgroup (distillation loss, sampling): any row length, stride and alignment.
+#pragma once
+
+#include "device_common.hpp"
+
+namespace alr {
+
+constexpr float LOG2E = 1.44269504088896340736f;
+
+// One row of V values of T, whose first value may sit anywhere within a 16-byte line: chunk c
+// holds the values [c * EPC - mis, c * EPC - mis + EPC) that exist.  Chunks that lie inside the
+// row are moved by one 16-byte access, the one or two at its ends value by value, so nothing
+// outside the row is touched.
+template <typename T>
+struct RowChunks {
+  static constexpr int EPC = 16 / (int)sizeof(T);
+  const T* p;
+  int V, mis, nch;
+
+  __device__ __forceinline__ RowChunks(const T* row, int V_) : p(row), V(V_) {
+    mis = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    nch = (V + mis + EPC - 1) / EPC;
+  }
+  __device__ __forceinline__ int first(int c) const { return c * EPC - mis; }
+  __device__ __forceinline__ bool inside(int c) const {
+    const int e0 = first(c);
+    return e0 >= 0 && e0 + EPC <= V;
+  }
+  // chunk c; -inf where it reaches past the row (all of it for c >= nch)
+  __device__ __forceinline__ u32x4 load(int c) const {
+    if (inside(c)) return *reinterpret_cast<const u32x4*>(p + first(c));
+    return edge(c);
+  }
+  __device__ u32x4 edge(int c) const {
+    u32x4 w;
+    const int e0 = first(c);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 4) {
+        const int e = e0 + k;
+        w[k] = e >= 0 && e < V ? __float_as_uint(p[e]) : 0xFF800000u;
+      } else {
+        const int a = e0 + 2 * k, b = a + 1;
+        const uint32_t lo = a >= 0 && a < V ? (uint32_t)p[a] : 0xFF80u;
+        const uint32_t hi = b >= 0 && b < V ? (uint32_t)p[b] : 0xFF80u;
+        w[k] = lo | hi << 16;
+      }
+    }
+    return w;
+  }
+  __device__ __forceinline__ float at(int e) const { return Elt<T>::ld(p + e); }
+};
+
+template <typename T>
+__device__ __forceinline__ void unpack(u32x4 w, float (&v)[RowChunks<T>::EPC]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (sizeof(T) == 4) {
+      v[k] = __uint_as_float(w[k]);
+    } else {
+      v[2 * k] = __uint_as_float(w[k] << 16);
+      v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+    }
+  }
+}
+
+// Writes chunk c of a row that `g` describes to the row `out`, rounded once to T; vec: out's chunks
+// are 16-byte aligned where g's are.
+template <typename T>
+__device__ __forceinline__ void store_chunk(const RowChunks<T>& g, T* out, bool vec, int c,
+                                            const float (&v)[RowChunks<T>::EPC]) {
+  constexpr int EPC = RowChunks<T>::EPC;
+  const int e0 = g.first(c);
+  if (vec && g.inside(c)) {
+    u32x4 w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 4)
+        w[k] = __float_as_uint(v[k]);
+      else
+        w[k] = pack2bf(v[2 * k], v[2 * k + 1]);
+    }
+    *reinterpret_cast<u32x4*>(out + e0) = w;
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < EPC; ++k)
+    if (e0 + k >= 0 && e0 + k < g.V) Elt<T>::st(out + e0 + k, v[k]);
+}
+
+}  // namespace alr

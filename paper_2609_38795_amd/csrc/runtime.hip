@@ -30,9 +30,12 @@
 #include "../../include/alr.h"
 #include "../../include/alr_debug.h"
 #include "attn_kernels.hpp"
+#include "distill_kernels.hpp"
 #include "gemm_kernels.hpp"
 #include "gemm_wide.hpp"
 #include "misc_kernels.hpp"
+#include "qk_norm_kernels.hpp"
+#include "sample_kernels.hpp"
 
 using namespace alr;
 
@@ -49,6 +52,7 @@ struct Layout {
   size_t w_embed, w_lm, w_fnorm;
   size_t layer0, layer_stride;  // per layer block
   size_t l_anorm, l_fnorm, l_qkv, l_o, l_gu, l_down;  // offsets within a layer block
+  size_t l_qnorm, l_knorm;
   size_t rope, rope_rows;
   size_t kc, vc, kv_layer_stride;
   size_t vt_stride;  // columns of the transposed V cache (0 when V is stored natural)
@@ -60,6 +64,7 @@ struct Layout {
   size_t i_pwork, i_dwork, i_maps, i_vtcol, i_vtpad, i_rowinfo, i_rowptr;
   size_t part_o, part_ml;
   size_t splitk, splitk_bytes;
+  size_t qk_part;
   size_t max_pwork, max_dwork, max_groups;
   size_t total;
 };
@@ -159,6 +164,8 @@ alr_status check_operand_sizes(const alr_config& c, const alr_limits& lim, char*
 
 // Partial sums of one 256x256 tile.
 constexpr size_t WIDE_PART_BYTES = 256 * 256 * 4;
+// Workgroups of the q/k norms' backward pass at most.
+constexpr int QK_BACK_WGS = 1024;
 // Up to this many rows a product may be cut into 8 K slices (pick_gemm).
 constexpr int FEW_ROWS = 256;
 
@@ -199,6 +206,8 @@ size_t compute_layout(const alr_config& c, const alr_limits& lim, Layout& L) {
     L.l_o = ltake(d * qd * es);
     L.l_gu = ltake(2 * F * d * es);
     L.l_down = ltake(d * F * es);
+    L.l_qnorm = ltake(hd * es);
+    L.l_knorm = ltake(hd * es);
     L.layer_stride = lo;
   }
   L.layer0 = take(nl * L.layer_stride);
@@ -264,6 +273,8 @@ size_t compute_layout(const alr_config& c, const alr_limits& lim, Layout& L) {
   L.splitk_bytes = std::max(4 * NA, 8 * std::min<size_t>(NA, FEW_ROWS)) *
                    std::max(qd + 2 * kvd, d) * 4;
   L.splitk = take(L.splitk_bytes);
+  // gain gradients of the q/k norms, one partial sum a workgroup
+  L.qk_part = take((size_t)QK_BACK_WGS * 2 * hd * 4);
   L.total = off;
   return off;
 }
@@ -325,6 +336,7 @@ struct alr_ctx {
   size_t ws_bytes;
   Layout L;
   bool prefilled = false;
+  bool qk_norm = false;  // alr_set_qk_norm: the layers norm q and k per head
   int n_cu = 256;  // compute units of the device (sizes the decode work split)
   float* splitk_buf = nullptr;  // split-K partial sums (workspace)
   char* noalloc_scratch = nullptr;  // device address of `scratch` on the context's device
@@ -349,7 +361,7 @@ struct alr_ctx {
   // least recently used first, and the private stream they are recorded and
   // replayed on, ordered after and before the caller's stream by two events
   struct RolloutGraph {
-    std::array<uintptr_t, 12> key;
+    std::array<uintptr_t, 18> key;
     hipGraphExec_t exec;
   };
   bool graphs_on = false;
@@ -875,6 +887,63 @@ void rope_pair_rows(int n, int hd, std::vector<int>& dst_of_src) {
   }
 }
 
+// RoPE rows of a pass over the corpus tokens (slot 0) or of rollout slot s
+RopeRows rope_rows(const alr_ctx* ctx, int s) {
+  const alr_config& c = ctx->cfg;
+  const int* ms = c.mrope_sections;
+  const bool none = ms[0] == 0 && ms[1] == 0 && ms[2] == 0;
+  const int half = c.head_dim / 2;
+  // null: with q/k norms the rotation reads the table itself, after the norm
+  f32x2* rows = ctx->qk_norm ? nullptr : ctx->at<f32x2>(ctx->L.rope_rows);
+  return RopeRows{rows, ctx->at<f32x2>(ctx->L.rope),
+                  ctx->at<int>(s == 0 ? ctx->L.i_tokpos : ctx->L.i_rpos), s, half,
+                  none ? half : ms[0], none ? half : ms[0] + ms[1]};
+}
+
+QkArgs qk_args(const alr_ctx* ctx, long n, int H, int G) {
+  const alr_config& c = ctx->cfg;
+  const int* ms = c.mrope_sections;
+  const bool none = ms[0] == 0 && ms[1] == 0 && ms[2] == 0;
+  QkArgs a = {};
+  a.tab = ctx->at<f32x2>(ctx->L.rope);
+  a.max_pos = c.max_pos;
+  a.hd = c.head_dim;
+  a.sec0 = none ? c.head_dim / 2 : ms[0];
+  a.sec01 = none ? c.head_dim / 2 : ms[0] + ms[1];
+  a.H = H;
+  a.G = G;
+  a.n = n;
+  a.eps = c.rms_eps;
+  return a;
+}
+
+template <typename T>
+void launch_qk(const QkArgs& a, hipStream_t st) {
+  const long wgs = (a.n * (a.H + a.G) + 3) / 4;
+  qk_norm_rope_any_kernel<T><<<(unsigned)std::min<long>(wgs, 1 << 22), 256, 0, st>>>(a);
+}
+
+template <typename T>
+void launch_qk_back(const alr_ctx* ctx, QkArgs a, float* dgq, float* dgk, hipStream_t st) {
+  const long wgs = (a.n * (a.H + a.G) + 3) / 4;
+  const int grid = (int)std::min<long>(wgs, QK_BACK_WGS);
+  a.part = ctx->at<float>(ctx->L.qk_part);
+  if (grid > 0) qk_norm_rope_back_any_kernel<T><<<grid, 256, 0, st>>>(a);
+  qk_gain_grad_kernel<<<(2 * a.hd + 31) / 32, 256, 0, st>>>(a.part, grid, a.hd, dgq, dgk);
+}
+
+template <typename T>
+void launch_distill(const DistillArgs& a, float* loss_out, hipStream_t st) {
+  const unsigned grid = (unsigned)std::min<long>(a.n, 1 << 20);
+  if (a.n > 0) {
+    if (a.dz)
+      distill_rows_kernel<T, 256, true><<<grid, 256, 0, st>>>(a);
+    else
+      distill_rows_kernel<T, 256, false><<<grid, 256, 0, st>>>(a);
+  }
+  distill_reduce_kernel<<<1, 1024, 0, st>>>(a.row_loss, a.weight, a.n, a.scale, loss_out);
+}
+
 // normed_in: the layer's input norm was already applied (fused into the
 // previous layer's down-projection reduce).  next_g / next_out: the RMSNorm
 // after this layer (the next layer's input norm or the final norm), which the
@@ -937,6 +1006,23 @@ alr_status layer_forward(alr_ctx* ctx, int l, int M, bool decode, int s, float* 
   else
     qkv(EpiQKV<T>{});
   ALR_LAUNCHED(ctx, "qkv gemm");
+  if (ctx->qk_norm) {
+    // the product left q and k as they are (its factor rows turn nothing), k in its cache place:
+    // both are normed and turned there.  In bf16 they are rounded once in between, as the
+    // normed input and every other product's operand are.
+    const RopeRows rr = rope_rows(ctx, s);
+    QkArgs a = qk_args(ctx, M, H, G);
+    a.q = a.q_out = qb;
+    a.q_rs = a.q_out_rs = qd;
+    a.k = a.k_out = decode ? kp + (long)(s - 1) * kvd : kc;
+    a.k_rs = a.k_out_rs = decode ? priv_rs : kvd;
+    a.gq = lw + L.l_qnorm;
+    a.gk = lw + L.l_knorm;
+    a.pos = rr.pos;
+    a.pos_add = rr.pos_add;
+    launch_qk<T>(a, st);
+    ALR_LAUNCHED(ctx, "q/k norm");
+  }
 
   const AttnGeom g = geom(c);
   {
@@ -1030,17 +1116,6 @@ alr_status layer_forward(alr_ctx* ctx, int l, int M, bool decode, int s, float* 
   return ALR_OK;
 }
 
-// RoPE rows of a pass over the corpus tokens (slot 0) or of rollout slot s
-RopeRows rope_rows(const alr_ctx* ctx, int s) {
-  const alr_config& c = ctx->cfg;
-  const int* ms = c.mrope_sections;
-  const bool none = ms[0] == 0 && ms[1] == 0 && ms[2] == 0;
-  const int half = c.head_dim / 2;
-  return RopeRows{ctx->at<f32x2>(ctx->L.rope_rows), ctx->at<f32x2>(ctx->L.rope),
-                  ctx->at<int>(s == 0 ? ctx->L.i_tokpos : ctx->L.i_rpos), s, half,
-                  none ? half : ms[0], none ? half : ms[0] + ms[1]};
-}
-
 int feat_index(const alr_config& c, int l) {
   for (int f = 0; f < c.n_feat; ++f)
     if (c.feat_layers[f] == l) return f;
@@ -1094,6 +1169,32 @@ alr_status prefill_impl(alr_ctx* ctx, int M, const int32_t* tokens, const void* 
   return ALR_OK;
 }
 
+SampleArgs sample_args(const alr_sampling* sp, const float* uniform, int V) {
+  SampleArgs a = {};
+  a.block = 1;
+  a.V = V;
+  int bits = 0;  // V <= 2^bits: whole weights below 2^(bits + shift) <= 2^62
+  while ((1 << bits) < V) ++bits;
+  a.shift = std::min(51, 62 - bits);
+  a.uniform = uniform;
+  if (sp) {
+    a.temperature = sp->temperature;
+    a.top_k = sp->top_k;
+    a.top_p = sp->top_p;
+    a.min_p = sp->min_p;
+  }
+  return a;
+}
+
+template <typename T>
+void launch_sample(const SampleArgs& a, hipStream_t st) {
+  const unsigned grid = (unsigned)std::min<long>(a.n, 1 << 20);
+  if (a.V > 8192)
+    sample_kernel<T, 1024><<<grid, 1024, 0, st>>>(a);
+  else
+    sample_kernel<T, 256><<<grid, 256, 0, st>>>(a);
+}
+
 // Output destinations of the labels of one rollout or corpus-label call.
 struct LabelDst {
   float* logprobs;  // [n, block, V] or null (then the logits go to the logit rows below)
@@ -1103,6 +1204,10 @@ struct LabelDst {
   float* tail;
   float* logit_rows = nullptr;      // [n, V] scratch for the logits; null: the workspace's
   LogitPart* part_rows = nullptr;   // [n, V/64] scratch for the partials; null: the workspace's
+  // sampled rollouts: `tokens` are drawn with these numbers instead of the argmax
+  const float* uniform = nullptr;          // [n, block]; null: greedy
+  const alr_sampling* sampling = nullptr;  // limits, or null: none
+  float* token_logp = nullptr;             // [n, block] or null
 };
 
 // Output head of slot s for the n sorted rows in xnorm: logits GEMM (into the
@@ -1142,13 +1247,31 @@ alr_status lm_head(alr_ctx* ctx, int n, int s, int block, const int* forced, con
   }
   launch_gemm<ALR_PROF_LM_GEMM, T>(ctx, ctx->at<T>(L.xnorm), d, ctx->at<T>(L.w_lm), d, n, V, d,
                                    el, st);
+  const bool sampled = rollout && out.uniform;
+  if (sampled) {  // from the raw logits: the finalisation may rewrite them
+    SampleArgs sa = sample_args(out.sampling, out.uniform, V);
+    sa.z = el.out;
+    sa.z_rs = el.rs;
+    sa.z_perm = el.perm != nullptr;
+    sa.perm = perm;
+    sa.block = block;
+    sa.s = s;
+    sa.n = n;
+    sa.forced = forced;
+    sa.next_tok = ctx->at<int>(L.i_cur);
+    sa.tokens = out.tokens;
+    sa.logp = out.token_logp;
+    launch_sample<float>(sa, st);
+    ALR_LAUNCHED(ctx, "sampling");
+    if (!out.top_ids && !out.logprobs) return ALR_OK;
+  }
   f.perm = perm;
   f.V = V;
   f.block = block;
   f.s = s;
-  f.tokens = out.tokens;
+  f.tokens = sampled ? nullptr : out.tokens;
   f.forced = rollout ? forced : nullptr;
-  f.next_tok = rollout ? ctx->at<int>(L.i_cur) : nullptr;
+  f.next_tok = rollout && !sampled ? ctx->at<int>(L.i_cur) : nullptr;
   f.top_ids = out.top_ids;
   f.top_logp = out.top_logp;
   f.tail = out.tail;
@@ -1242,11 +1365,15 @@ alr_status run_rollout(alr_ctx* ctx, int n, int block, const int32_t* forced, co
   if (cap != hipStreamCaptureStatusNone)
     return rollout_impl<T>(ctx, n, block, forced, out, feats_out, st);
   hipStream_t gs = ctx->graph_stream;  // created by alr_set_rollout_graphs
-  const std::array<uintptr_t, 12> key{
+  const alr_sampling sp = out.sampling ? *out.sampling : alr_sampling{};
+  const std::array<uintptr_t, 18> key{
       (uintptr_t)n, (uintptr_t)block, (uintptr_t)ctx->h_dwork.size(), (uintptr_t)forced,
       (uintptr_t)feats_out, (uintptr_t)out.logprobs, (uintptr_t)out.tokens,
       (uintptr_t)out.top_ids, (uintptr_t)out.top_logp, (uintptr_t)out.tail,
-      (uintptr_t)out.logit_rows, (uintptr_t)out.part_rows};
+      (uintptr_t)out.logit_rows, (uintptr_t)out.part_rows,
+      // uniform is set where a sampled rollout is asked for, and there only
+      (uintptr_t)out.uniform, (uintptr_t)out.token_logp, (uintptr_t)sp.temperature,
+      (uintptr_t)sp.top_k, (uintptr_t)sp.top_p, (uintptr_t)sp.min_p};
   ALR_HIP(ctx, hipEventRecord(ctx->graph_in, st));
   ALR_HIP(ctx, hipStreamWaitEvent(gs, ctx->graph_in, 0));
   hipGraphExec_t exec = nullptr;
@@ -2015,6 +2142,274 @@ alr_status alr_corpus_labels(alr_ctx* ctx, int32_t n_anchor, const int32_t* anch
                                  gate_hard_out, s)
              : corpus_impl<float>(ctx, n_anchor, block, out, corpus_logp_out, gate_soft_out,
                                   gate_hard_out, s);
+}
+
+alr_status alr_rollout_sampled(alr_ctx* ctx, int32_t n_anchor, const int32_t* anchor_seq,
+                               const int32_t* anchor_pos, int32_t block,
+                               const alr_sampling* sampling, const float* uniform,
+                               const int32_t* forced, int32_t* tokens_out, float* token_logp_out,
+                               int32_t* top_ids_out, float* top_logp_out, float* tail_out,
+                               float* logprobs_out, float* feats_out, alr_stream stream) {
+  if (!ctx) return ALR_E_INVALID_ARG;
+  if (!uniform || !tokens_out)
+    return fail(ctx, ALR_E_INVALID_ARG, "uniform and tokens_out must not be NULL");
+  if ((top_ids_out == nullptr) != (top_logp_out == nullptr) ||
+      (top_ids_out == nullptr) != (tail_out == nullptr))
+    return fail(ctx, ALR_E_INVALID_ARG,
+                "top_ids_out, top_logp_out and tail_out must all be given or all be NULL");
+  if (ctx->cfg.vocab > ALR_SAMPLE_MAX_VOCAB)
+    return fail(ctx, ALR_E_UNSUPPORTED, "vocab %d > %d", ctx->cfg.vocab, ALR_SAMPLE_MAX_VOCAB);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  alr_status st = prepare_anchors(ctx, n_anchor, anchor_seq, anchor_pos, block, true, s);
+  if (st != ALR_OK) return st;
+  LabelDst out{logprobs_out, tokens_out, top_ids_out, top_logp_out, tail_out};
+  out.uniform = uniform;
+  out.sampling = sampling;
+  out.token_logp = token_logp_out;
+  return (ctx->cfg.dtype == ALR_BF16)
+             ? run_rollout<bf16>(ctx, n_anchor, block, forced, out, feats_out, s, true)
+             : run_rollout<float>(ctx, n_anchor, block, forced, out, feats_out, s, true);
+}
+
+namespace {
+
+// Checks that the operators over rows of logits share.
+alr_status check_logits(alr_ctx* ctx, int32_t n, int32_t vocab, const void* logits, int32_t dtype,
+                        int64_t row_stride) {
+  if (n < 0 || vocab < 1) return fail(ctx, ALR_E_INVALID_ARG, "n %d / vocab %d invalid", n, vocab);
+  if (dtype != ALR_F32 && dtype != ALR_BF16)
+    return fail(ctx, ALR_E_INVALID_ARG, "dtype %d is not ALR_F32 or ALR_BF16", dtype);
+  if (n > 0 && !logits) return fail(ctx, ALR_E_INVALID_ARG, "logits is NULL");
+  if (reinterpret_cast<uintptr_t>(logits) % (dtype == ALR_F32 ? 4 : 2))
+    return fail(ctx, ALR_E_INVALID_ARG, "logits is not aligned to its elements");
+  if (row_stride < vocab)
+    return fail(ctx, ALR_E_INVALID_ARG, "row stride %lld < vocab %d", (long long)row_stride, vocab);
+  return ALR_OK;
+}
+
+}  // namespace
+
+alr_status alr_sample(alr_ctx* ctx, int32_t n, int32_t vocab, const void* logits, int32_t dtype,
+                      int64_t row_stride, const alr_sampling* sampling, const float* uniform,
+                      int32_t* tokens_out, float* logp_out, alr_stream stream) {
+  if (!ctx) return ALR_E_INVALID_ARG;
+  const alr_status st = check_logits(ctx, n, vocab, logits, dtype, row_stride);
+  if (st != ALR_OK) return st;
+  if (vocab > ALR_SAMPLE_MAX_VOCAB)
+    return fail(ctx, ALR_E_UNSUPPORTED, "vocab %d > %d", vocab, ALR_SAMPLE_MAX_VOCAB);
+  if (n == 0) return ALR_OK;
+  if (!uniform || !tokens_out)
+    return fail(ctx, ALR_E_INVALID_ARG, "uniform and tokens_out must not be NULL");
+  SampleArgs a = sample_args(sampling, uniform, vocab);
+  a.z = logits;
+  a.z_rs = (long)row_stride;
+  a.n = n;
+  a.tokens = tokens_out;
+  a.logp = logp_out;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (dtype == ALR_BF16)
+    launch_sample<bf16>(a, s);
+  else
+    launch_sample<float>(a, s);
+  ALR_LAUNCHED(ctx, "sampling");
+  return ALR_OK;
+}
+
+alr_status alr_distill_loss(alr_ctx* ctx, int32_t n, int32_t vocab, const void* logits,
+                            int32_t dtype, int64_t row_stride, const int32_t* top_ids,
+                            const float* top_logp, const float* tail, const float* weight,
+                            float scale, const float* grad_out, float* loss_out,
+                            float* row_loss_out, void* dlogits_out, int64_t dlogits_stride,
+                            alr_stream stream) {
+  if (!ctx) return ALR_E_INVALID_ARG;
+  const alr_status st = check_logits(ctx, n, vocab, logits, dtype, row_stride);
+  if (st != ALR_OK) return st;
+  if (!loss_out) return fail(ctx, ALR_E_INVALID_ARG, "loss_out is NULL");
+  if (n > 0 && (!top_ids || !top_logp || !tail || !row_loss_out))
+    return fail(ctx, ALR_E_INVALID_ARG,
+                "top_ids, top_logp, tail and row_loss_out must not be NULL");
+  if (dlogits_out) {
+    if (reinterpret_cast<uintptr_t>(dlogits_out) % (dtype == ALR_F32 ? 4 : 2))
+      return fail(ctx, ALR_E_INVALID_ARG, "dlogits_out is not aligned to its elements");
+    if (dlogits_stride < vocab)
+      return fail(ctx, ALR_E_INVALID_ARG, "dlogits stride %lld < vocab %d",
+                  (long long)dlogits_stride, vocab);
+    if (dlogits_out == logits && n > 1 && dlogits_stride != row_stride)
+      return fail(ctx, ALR_E_INVALID_ARG, "gradients in place of the logits need their row stride");
+  }
+  DistillArgs a = {};
+  a.z = logits;
+  a.z_rs = (long)row_stride;
+  a.ids = top_ids;
+  a.logp = top_logp;
+  a.tail = tail;
+  a.weight = weight;
+  a.up = grad_out;
+  a.scale = scale;
+  a.n = n;
+  a.V = vocab;
+  a.row_loss = row_loss_out;
+  a.dz = dlogits_out;
+  a.dz_rs = (long)dlogits_stride;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (dtype == ALR_BF16)
+    launch_distill<bf16>(a, loss_out, s);
+  else
+    launch_distill<float>(a, loss_out, s);
+  ALR_LAUNCHED(ctx, "distillation loss");
+  return ALR_OK;
+}
+
+namespace {
+
+// One of the two (rows of heads, their gain, their output) of a q/k norm call.
+alr_status check_heads(alr_ctx* ctx, const char* name, int32_t heads, const void* const* ptrs,
+                       int n_ptrs, const int64_t* strides, int n_strides) {
+  if (heads == 0) return ALR_OK;
+  const int es = ctx->cfg.dtype == ALR_BF16 ? 2 : 4;
+  for (int i = 0; i < n_ptrs; ++i) {
+    if (!ptrs[i]) return fail(ctx, ALR_E_INVALID_ARG, "a pointer of %s is NULL", name);
+    if (reinterpret_cast<uintptr_t>(ptrs[i]) % es)
+      return fail(ctx, ALR_E_INVALID_ARG, "a pointer of %s is not aligned to its elements", name);
+  }
+  for (int i = 0; i < n_strides; ++i)
+    if (strides[i] < (int64_t)heads * ctx->cfg.head_dim)
+      return fail(ctx, ALR_E_INVALID_ARG, "a row stride of %s, %lld, is below %d heads x %d", name,
+                  (long long)strides[i], heads, ctx->cfg.head_dim);
+  return ALR_OK;
+}
+
+alr_status check_qk(alr_ctx* ctx, int32_t n, int32_t q_heads, int32_t k_heads,
+                    const int32_t* positions) {
+  if (n < 0 || q_heads < 0 || k_heads < 0 || q_heads + (int64_t)k_heads < 1 ||
+      q_heads + (int64_t)k_heads > 65535)
+    return fail(ctx, ALR_E_INVALID_ARG, "n %d / heads %d and %d invalid", n, q_heads, k_heads);
+  if (!positions && n > ctx->cfg.max_pos)
+    return fail(ctx, ALR_E_OUT_OF_RANGE, "row %d as its own position >= max_pos %d", n - 1,
+                ctx->cfg.max_pos);
+  return ALR_OK;
+}
+
+}  // namespace
+
+alr_status alr_qk_norm_rope(alr_ctx* ctx, int32_t n, int32_t q_heads, int32_t k_heads,
+                            const int32_t* positions, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const void* q_gain,
+                            const void* k_gain, void* q_out, int64_t q_out_stride, void* k_out,
+                            int64_t k_out_stride, alr_stream stream) {
+  if (!ctx) return ALR_E_INVALID_ARG;
+  alr_status st = check_qk(ctx, n, q_heads, k_heads, positions);
+  if (st != ALR_OK) return st;
+  if (n == 0) return ALR_OK;
+  const void* qp[] = {q, q_gain, q_out};
+  const void* kp[] = {k, k_gain, k_out};
+  const int64_t qs[] = {q_stride, q_out_stride}, ks[] = {k_stride, k_out_stride};
+  st = check_heads(ctx, "q", q_heads, qp, 3, qs, 2);
+  if (st == ALR_OK) st = check_heads(ctx, "k", k_heads, kp, 3, ks, 2);
+  if (st != ALR_OK) return st;
+  QkArgs a = qk_args(ctx, n, q_heads, k_heads);
+  a.q = q;
+  a.q_rs = (long)q_stride;
+  a.k = k;
+  a.k_rs = (long)k_stride;
+  a.gq = q_gain;
+  a.gk = k_gain;
+  a.q_out = q_out;
+  a.q_out_rs = (long)q_out_stride;
+  a.k_out = k_out;
+  a.k_out_rs = (long)k_out_stride;
+  a.pos = positions;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (ctx->cfg.dtype == ALR_BF16)
+    launch_qk<bf16>(a, s);
+  else
+    launch_qk<float>(a, s);
+  ALR_LAUNCHED(ctx, "q/k norm");
+  return ALR_OK;
+}
+
+alr_status alr_qk_norm_rope_backward(alr_ctx* ctx, int32_t n, int32_t q_heads, int32_t k_heads,
+                                     const int32_t* positions, const void* q, int64_t q_stride,
+                                     const void* k, int64_t k_stride, const void* q_gain,
+                                     const void* k_gain, const void* dq_out, int64_t dq_out_stride,
+                                     const void* dk_out, int64_t dk_out_stride, void* dq,
+                                     int64_t dq_stride, void* dk, int64_t dk_stride,
+                                     float* dq_gain, float* dk_gain, alr_stream stream) {
+  if (!ctx) return ALR_E_INVALID_ARG;
+  alr_status st = check_qk(ctx, n, q_heads, k_heads, positions);
+  if (st != ALR_OK) return st;
+  if (q_heads > 0 && !dq_gain) return fail(ctx, ALR_E_INVALID_ARG, "dq_gain is NULL");
+  if (k_heads > 0 && !dk_gain) return fail(ctx, ALR_E_INVALID_ARG, "dk_gain is NULL");
+  if (n > 0) {
+    const void* qp[] = {q, q_gain, dq_out, dq};
+    const void* kp[] = {k, k_gain, dk_out, dk};
+    const int64_t qs[] = {q_stride, dq_out_stride, dq_stride};
+    const int64_t ks[] = {k_stride, dk_out_stride, dk_stride};
+    st = check_heads(ctx, "q", q_heads, qp, 4, qs, 3);
+    if (st == ALR_OK) st = check_heads(ctx, "k", k_heads, kp, 4, ks, 3);
+    if (st != ALR_OK) return st;
+  }
+  QkArgs a = qk_args(ctx, n, q_heads, k_heads);
+  a.q = q;
+  a.q_rs = (long)q_stride;
+  a.k = k;
+  a.k_rs = (long)k_stride;
+  a.gq = q_gain;
+  a.gk = k_gain;
+  a.dq_in = dq_out;
+  a.dq_in_rs = (long)dq_out_stride;
+  a.dk_in = dk_out;
+  a.dk_in_rs = (long)dk_out_stride;
+  a.q_out = dq;
+  a.q_out_rs = (long)dq_stride;
+  a.k_out = dk;
+  a.k_out_rs = (long)dk_stride;
+  a.pos = positions;
+  float* const dgq = q_heads > 0 ? dq_gain : nullptr;
+  float* const dgk = k_heads > 0 ? dk_gain : nullptr;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (ctx->cfg.dtype == ALR_BF16)
+    launch_qk_back<bf16>(ctx, a, dgq, dgk, s);
+  else
+    launch_qk_back<float>(ctx, a, dgq, dgk, s);
+  ALR_LAUNCHED(ctx, "q/k norm gradients");
+  return ALR_OK;
+}
+
+alr_status alr_set_qk_norm(alr_ctx* ctx, const void* const* q_gain, const void* const* k_gain,
+                           alr_stream stream) {
+  if (!ctx) return ALR_E_INVALID_ARG;
+  if ((q_gain == nullptr) != (k_gain == nullptr))
+    return fail(ctx, ALR_E_INVALID_ARG, "q_gain and k_gain must both be given or both be NULL");
+  const alr_config& c = ctx->cfg;
+  const Layout& L = ctx->L;
+  if (q_gain)
+    for (int l = 0; l < c.n_layers; ++l)
+      if (!q_gain[l] || !k_gain[l])
+        return fail(ctx, ALR_E_INVALID_ARG, "q/k norm gains of layer %d incomplete", l);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  ALR_HIP(ctx, hipStreamIsCapturing(s, &cap));
+  if (cap != hipStreamCaptureStatusNone)
+    return fail(ctx, ALR_E_STATE, "the q/k norms cannot be changed in a captured graph");
+  drop_rollout_graphs(ctx);
+  ctx->prefilled = false;  // the cache holds keys of the other kind
+  ctx->qk_norm = false;
+  if (!q_gain) return ALR_OK;
+  const size_t bytes = (size_t)c.head_dim * L.es;
+  for (int l = 0; l < c.n_layers; ++l) {
+    ALR_HIP(ctx, hipMemcpyAsync(ctx->layer(l) + L.l_qnorm, q_gain[l], bytes,
+                                hipMemcpyDeviceToDevice, s));
+    ALR_HIP(ctx, hipMemcpyAsync(ctx->layer(l) + L.l_knorm, k_gain[l], bytes,
+                                hipMemcpyDeviceToDevice, s));
+  }
+  const long rows = std::max(ctx->lim.max_tokens, ctx->lim.max_anchors);
+  const long vals = rows * (c.head_dim / 2);
+  unit_factor_kernel<<<(unsigned)((vals + 255) / 256), 256, 0, s>>>(ctx->at<f32x2>(L.rope_rows),
+                                                                   vals);
+  ALR_LAUNCHED(ctx, "unit factors");
+  ctx->qk_norm = true;
+  return ALR_OK;
 }
 
 alr_status alr_ira_assemble(alr_ctx* ctx, int32_t n_primary, int32_t block,
