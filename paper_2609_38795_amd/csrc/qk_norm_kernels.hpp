@@ -153,24 +153,284 @@ __global__ __launch_bounds__(256) void qk_norm_rope_back_any_kernel(QkArgs a) {
   for (int i = threadIdx.x; i < 2 * a.hd; i += 256) out[i] = sum[i / a.hd][i % a.hd];
 }
 
-// Gain gradients: the workgroups' partial sums added in order of the workgroups, 32 columns a
-// workgroup, its 8 thread rows taking every 8th partial and meeting at the end.
-__global__ __launch_bounds__(256) void qk_gain_grad_kernel(const float* __restrict__ part, int n_wg,
-                                                           int hd, float* __restrict__ dgq,
-                                                           float* __restrict__ dgk) {
-  __shared__ float s[8][32];
-  const int col = threadIdx.x & 31, sub = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
+// Sum over each aligned group of LPH lanes, the same in all of them (DPP permutations as group_sum).
+template <int LPH>
+__device__ __forceinline__ float head_sum(float v) {
+  if constexpr (LPH == 32) v = sum_xor16(v);
+  if constexpr (LPH >= 16) v += dpp_perm<0x140>(v);
+  if constexpr (LPH >= 8) v += dpp_perm<0x141>(v);
+  if constexpr (LPH >= 2) v += dpp_perm<0xB1>(v);
+  if constexpr (LPH >= 4) v += dpp_perm<0x4E>(v);
+  return v;
+}
+
+// Heads whose half is whole 16-byte runs, in rows on 16-byte boundaries: LPH lanes per head, each with
+// one run of VEC values of the low half and the one that is turned with it, 64 / LPH heads of a row at a
+// time.  The factors of the row's position are read once per wave, and the loads of U such steps go out before
+// the first use.
+template <typename T, int LPH>
+struct QkLane {
+  static constexpr int VEC = 16 / (int)sizeof(T), HPW = 64 / LPH;
+  int j0, head;  // the lane's first index within the half; its head within a step
+  bool on;       // lanes past the half idle (halves of 5 or 6 runs)
+  __device__ __forceinline__ explicit QkLane(int half) {
+    const int lane = threadIdx.x & 63;
+    j0 = (lane & (LPH - 1)) * VEC;
+    head = lane / LPH;
+    on = j0 < half;
+  }
+  __device__ __forceinline__ static void widen(u32x4 w, float (&v)[VEC]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 4) {
+        v[k] = __uint_as_float(w[k]);
+      } else {
+        v[2 * k] = __uint_as_float(w[k] << 16);
+        v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+      }
+    }
+  }
+  __device__ __forceinline__ static u32x4 narrow(const float (&v)[VEC]) {
+    u32x4 w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 4)
+        w[k] = __float_as_uint(v[k]);
+      else
+        w[k] = pack2bf(v[2 * k], v[2 * k + 1]);
+    }
+    return w;
+  }
+  __device__ __forceinline__ u32x4 run(const T* p) const {
+    return on ? *reinterpret_cast<const u32x4*>(p) : u32x4{0, 0, 0, 0};
+  }
+  // (cos, sin) of row r at the lane's run
+  __device__ __forceinline__ void factors(const QkArgs& a, long r, float (&cs)[VEC],
+                                          float (&sn)[VEC]) const {
+    const int i1 = j0 + VEC - 1;
+    const bool one_axis = (j0 < a.sec0) == (i1 < a.sec0) && (j0 < a.sec01) == (i1 < a.sec01);
+    if (!on) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) cs[e] = 1.f, sn[e] = 0.f;
+    } else if (one_axis) {
+      const int axis = j0 < a.sec0 ? 0 : j0 < a.sec01 ? 1 : 2;
+      const long p = (a.pos ? (long)a.pos[3 * r + axis] : r) + a.pos_add;
+      const bool ok = p >= 0 && p < a.max_pos;
+      const float bad = __builtin_nanf("");
+      const f32x4* t = reinterpret_cast<const f32x4*>(a.tab + (ok ? p : 0) * (a.hd >> 1) + j0);
+#pragma unroll
+      for (int e = 0; e < VEC / 2; ++e) {
+        const f32x4 w = t[e];
+        cs[2 * e] = ok ? w[0] : bad;
+        sn[2 * e] = w[1];
+        cs[2 * e + 1] = ok ? w[2] : bad;
+        sn[2 * e + 1] = w[3];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const f32x2 w = qk_factor(a, r, j0 + e);
+        cs[e] = w[0];
+        sn[e] = w[1];
+      }
+    }
+  }
+};
+
+// A row's heads come as steps of HPW heads, those of q and then those of k; a wave takes the steps
+// [part * per, (part + 1) * per) of one row.
+struct QkSteps {
+  int q, k, per, splits;  // steps of q and of k; steps and parts of a row
+};
+
+template <typename T, int LPH>
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a, QkSteps st) {
+  using L = QkLane<T, LPH>;
+  constexpr int VEC = L::VEC, U = 4;
+  const int half = a.hd >> 1;
+  const L ln(half);
+  const long units = a.n * st.splits;
+  for (long unit = (long)blockIdx.x * 4 + (threadIdx.x >> 6); unit < units;
+       unit += (long)gridDim.x * 4) {
+    const long r = unit / st.splits;
+    const int s0 = (int)(unit - r * st.splits) * st.per, s1 = min(s0 + st.per, st.q + st.k);
+    float cs[VEC], sn[VEC];
+    ln.factors(a, r, cs, sn);
+    auto steps = [&](int b, int e, int heads, const T* x, T* y, const T* g) {
+      if (b >= e) return;
+      float glo[VEC], ghi[VEC];
+      L::widen(ln.run(g + ln.j0), glo);
+      L::widen(ln.run(g + ln.j0 + half), ghi);
+      for (int s = b; s < e; s += U) {
+        u32x4 lo[U], hi[U];
+  #pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int h = (s + u) * L::HPW + ln.head;
+          const bool in = s + u < e && h < heads;
+          const T* p = x + (long)(in ? h : 0) * a.hd + ln.j0;
+          lo[u] = in ? ln.run(p) : u32x4{0, 0, 0, 0};
+          hi[u] = in ? ln.run(p + half) : u32x4{0, 0, 0, 0};
+        }
+  #pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (s + u >= e) break;
+          const int h = (s + u) * L::HPW + ln.head;
+          float l[VEC], m[VEC], ss = 0.f;
+          L::widen(lo[u], l);
+          L::widen(hi[u], m);
+  #pragma unroll
+          for (int k = 0; k < VEC; ++k) ss = fmaf(l[k], l[k], fmaf(m[k], m[k], ss));
+          const float inv = 1.0f / sqrtf(head_sum<LPH>(ss) / (float)a.hd + a.eps);
+          float yl[VEC], yh[VEC];
+  #pragma unroll
+          for (int k = 0; k < VEC; ++k) {
+            const float nl = l[k] * inv * glo[k], nh = m[k] * inv * ghi[k];
+            yl[k] = rope_a(nl, nh, cs[k], sn[k]);
+            yh[k] = rope_b(nl, nh, cs[k], sn[k]);
+          }
+          if (h < heads && ln.on) {
+            T* o = y + (long)h * a.hd + ln.j0;
+            *reinterpret_cast<u32x4*>(o) = L::narrow(yl);
+            *reinterpret_cast<u32x4*>(o + half) = L::narrow(yh);
+          }
+        }
+      }
+    };
+    steps(s0, min(s1, st.q), a.H, static_cast<const T*>(a.q) + r * a.q_rs,
+          static_cast<T*>(a.q_out) + r * a.q_out_rs, static_cast<const T*>(a.gq));
+    steps(max(s0 - st.q, 0), s1 - st.q, a.G, static_cast<const T*>(a.k) + r * a.k_rs,
+          static_cast<T*>(a.k_out) + r * a.k_out_rs, static_cast<const T*>(a.gk));
+  }
+}
+
+// Backward: the grid's waves walk the (row, part) units; a lane keeps the gain gradients of its runs in
+// registers until the end, then the heads of a wave meet by shuffles and the waves in LDS.
+template <typename T, int LPH>
+__global__ __launch_bounds__(256) void qk_norm_rope_back_kernel(QkArgs a, QkSteps st) {
+  using L = QkLane<T, LPH>;
+  constexpr int VEC = L::VEC;
+  __shared__ float sum[4][2][256];
+  const int half = a.hd >> 1, wave = threadIdx.x >> 6;
+  const L ln(half);
+  float dg[2][2][VEC] = {};  // [q, k][low, high]
+  const long units = a.n * st.splits;
+  for (long unit = (long)blockIdx.x * 4 + wave; unit < units; unit += (long)gridDim.x * 4) {
+    const long r = unit / st.splits;
+    const int s0 = (int)(unit - r * st.splits) * st.per, s1 = min(s0 + st.per, st.q + st.k);
+    float cs[VEC], sn[VEC];
+    ln.factors(a, r, cs, sn);
+    auto steps = [&](int b, int e, int heads, const T* x, const T* dy, T* dx, const T* g,
+                     float (&acc)[2][VEC]) {
+      constexpr int U = 2;
+      if (b >= e) return;
+      float gain[2][VEC];
+      L::widen(ln.run(g + ln.j0), gain[0]);
+      L::widen(ln.run(g + ln.j0 + half), gain[1]);
+      for (int s = b; s < e; s += U) {
+        u32x4 wx[U][2], wd[U][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int h = (s + u) * L::HPW + ln.head;
+          const bool in = s + u < e && h < heads;
+          const long at = (long)(in ? h : 0) * a.hd + ln.j0;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            wx[u][t] = in ? ln.run(x + at + t * half) : u32x4{0, 0, 0, 0};
+            wd[u][t] = in ? ln.run(dy + at + t * half) : u32x4{0, 0, 0, 0};
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (s + u >= e) break;
+          const int h = (s + u) * L::HPW + ln.head;
+          float xv[2][VEC], d[2][VEC], lo[VEC], hi[VEC], ss = 0.f;
+          L::widen(wx[u][0], xv[0]);
+          L::widen(wx[u][1], xv[1]);
+          L::widen(wd[u][0], lo);
+          L::widen(wd[u][1], hi);
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) {
+            d[0][k] = rope_a(lo[k], hi[k], cs[k], -sn[k]);
+            d[1][k] = rope_b(lo[k], hi[k], cs[k], -sn[k]);
+            ss = fmaf(xv[0][k], xv[0][k], fmaf(xv[1][k], xv[1][k], ss));
+          }
+          const float inv = 1.0f / sqrtf(head_sum<LPH>(ss) / (float)a.hd + a.eps);
+          float dot = 0.f;
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+              xv[t][k] *= inv;
+              acc[t][k] = fmaf(d[t][k], xv[t][k], acc[t][k]);
+              d[t][k] *= gain[t][k];
+              dot = fmaf(d[t][k], xv[t][k], dot);
+            }
+          dot = head_sum<LPH>(dot) / (float)a.hd;
+          if (h < heads && ln.on) {
+            T* o = dx + (long)h * a.hd + ln.j0;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+              for (int k = 0; k < VEC; ++k) d[t][k] = inv * (d[t][k] - xv[t][k] * dot);
+              *reinterpret_cast<u32x4*>(o + t * half) = L::narrow(d[t]);
+            }
+          }
+        }
+      }
+    };
+    steps(s0, min(s1, st.q), a.H, static_cast<const T*>(a.q) + r * a.q_rs,
+          static_cast<const T*>(a.dq_in) + r * a.dq_in_rs, static_cast<T*>(a.q_out) + r * a.q_out_rs,
+          static_cast<const T*>(a.gq), dg[0]);
+    steps(max(s0 - st.q, 0), s1 - st.q, a.G, static_cast<const T*>(a.k) + r * a.k_rs,
+          static_cast<const T*>(a.dk_in) + r * a.dk_in_rs, static_cast<T*>(a.k_out) + r * a.k_out_rs,
+          static_cast<const T*>(a.gk), dg[1]);
+  }
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        float v = dg[b][t][k];
+#pragma unroll
+        for (int o = LPH; o < 64; o <<= 1) v += __shfl_xor(v, o);
+        if (ln.head == 0 && ln.on) sum[wave][b][t * half + ln.j0 + k] = v;
+      }
+  __syncthreads();
+  float* out = a.part + (long)blockIdx.x * 2 * a.hd;
+  for (int i = threadIdx.x; i < 2 * a.hd; i += 256) {
+    const int b = i / a.hd, c = i - b * a.hd;
+    out[i] = ((sum[0][b][c] + sum[1][b][c]) + sum[2][b][c]) + sum[3][b][c];
+  }
+}
+
+// Gain gradients: the workgroups' partial sums, 16 columns a workgroup; each of its 64 thread rows takes
+// every 64th partial, four loads in flight, and they meet in LDS in order.
+__global__ __launch_bounds__(1024) void qk_gain_grad_kernel(const float* __restrict__ part, int n_wg,
+                                                            int hd, float* __restrict__ dgq,
+                                                            float* __restrict__ dgk) {
+  __shared__ float s[64][17];
+  const int col = threadIdx.x & 15, sub = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
   float t = 0.f;
   if (c < 2 * hd)
-    for (int w = sub; w < n_wg; w += 8) t += part[(long)w * 2 * hd + c];
+    for (int w = sub; w < n_wg; w += 256) {
+      float v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        v[u] = w + 64 * u < n_wg ? part[(long)(w + 64 * u) * 2 * hd + c] : 0.f;
+      t += ((v[0] + v[1]) + v[2]) + v[3];
+    }
   s[sub][col] = t;
   __syncthreads();
+  for (int half = 32; half > 0; half >>= 1) {
+    if (sub < half) s[sub][col] += s[sub + half][col];
+    __syncthreads();
+  }
   if (sub != 0 || c >= 2 * hd) return;
-  for (int i = 1; i < 8; ++i) t += s[i][col];
   if (c < hd) {
-    if (dgq) dgq[c] = t;
+    if (dgq) dgq[c] = s[0][col];
   } else if (dgk) {
-    dgk[c - hd] = t;
+    dgk[c - hd] = s[0][col];
   }
 }
 

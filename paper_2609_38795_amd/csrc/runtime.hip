@@ -917,19 +917,70 @@ QkArgs qk_args(const alr_ctx* ctx, long n, int H, int G) {
   return a;
 }
 
+// Whether every row of a q/k norm call is whole 16-byte runs on 16-byte boundaries (what
+// qk_norm_rope_kernel and its backward form move); else the kernels of one value at a time.
 template <typename T>
-void launch_qk(const QkArgs& a, hipStream_t st) {
-  const long wgs = (a.n * (a.H + a.G) + 3) / 4;
-  qk_norm_rope_any_kernel<T><<<(unsigned)std::min<long>(wgs, 1 << 22), 256, 0, st>>>(a);
+bool qk_in_runs(const QkArgs& a, bool back) {
+  constexpr long VEC = 16 / sizeof(T);
+  if (a.hd % (2 * VEC)) return false;
+  auto rows = [&](int heads, const void* p, long rs) {
+    return heads == 0 || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && rs % VEC == 0);
+  };
+  return rows(a.H, a.q, a.q_rs) && rows(a.G, a.k, a.k_rs) && rows(a.H, a.q_out, a.q_out_rs) &&
+         rows(a.G, a.k_out, a.k_out_rs) && rows(a.H, a.gq, 0) && rows(a.G, a.gk, 0) &&
+         (!back || (rows(a.H, a.dq_in, a.dq_in_rs) && rows(a.G, a.dk_in, a.dk_in_rs)));
+}
+
+// f(lanes per head as a constant, steps): the smallest power of two of lanes that holds half a head,
+// and a row's steps in as many parts as it takes to have `waves` of them.
+template <typename T, typename F>
+void qk_lanes(const QkArgs& a, long waves, F f) {
+  const int runs = a.hd / 2 / (16 / (int)sizeof(T));
+  auto go = [&](auto lph) {
+    constexpr int HPW = 64 / decltype(lph)::value;
+    QkSteps st;
+    st.q = (a.H + HPW - 1) / HPW;
+    st.k = (a.G + HPW - 1) / HPW;
+    const int all = st.q + st.k;
+    const long want = std::max<long>(1, std::min<long>(all, waves / std::max<long>(1, a.n)));
+    st.per = (int)((all + want - 1) / want);
+    st.splits = (all + st.per - 1) / st.per;
+    f(lph, st);
+  };
+  if (runs <= 2) go(std::integral_constant<int, 2>{});
+  else if (runs <= 4) go(std::integral_constant<int, 4>{});
+  else if (runs <= 8) go(std::integral_constant<int, 8>{});
+  else if (runs <= 16) go(std::integral_constant<int, 16>{});
+  else go(std::integral_constant<int, 32>{});
+}
+
+template <typename T>
+void launch_qk(const alr_ctx* ctx, const QkArgs& a, hipStream_t st) {
+  if (!qk_in_runs<T>(a, false)) {
+    const long wgs = (a.n * (a.H + a.G) + 3) / 4;
+    qk_norm_rope_any_kernel<T><<<(unsigned)std::min<long>(wgs, 1 << 22), 256, 0, st>>>(a);
+    return;
+  }
+  qk_lanes<T>(a, 8L * ctx->n_cu, [&](auto lph, QkSteps steps) {
+    const long wgs = std::min<long>((a.n * steps.splits + 3) / 4, 1 << 22);
+    qk_norm_rope_kernel<T, decltype(lph)::value><<<(unsigned)wgs, 256, 0, st>>>(a, steps);
+  });
 }
 
 template <typename T>
 void launch_qk_back(const alr_ctx* ctx, QkArgs a, float* dgq, float* dgk, hipStream_t st) {
-  const long wgs = (a.n * (a.H + a.G) + 3) / 4;
-  const int grid = (int)std::min<long>(wgs, QK_BACK_WGS);
   a.part = ctx->at<float>(ctx->L.qk_part);
-  if (grid > 0) qk_norm_rope_back_any_kernel<T><<<grid, 256, 0, st>>>(a);
-  qk_gain_grad_kernel<<<(2 * a.hd + 31) / 32, 256, 0, st>>>(a.part, grid, a.hd, dgq, dgk);
+  int grid = 0;
+  if (a.n > 0 && !qk_in_runs<T>(a, true)) {
+    grid = (int)std::min<long>((a.n * (a.H + a.G) + 3) / 4, QK_BACK_WGS);
+    qk_norm_rope_back_any_kernel<T><<<grid, 256, 0, st>>>(a);
+  } else if (a.n > 0) {
+    qk_lanes<T>(a, 8L * ctx->n_cu, [&](auto lph, QkSteps steps) {
+      grid = (int)std::min<long>((a.n * steps.splits + 3) / 4, QK_BACK_WGS);
+      qk_norm_rope_back_kernel<T, decltype(lph)::value><<<grid, 256, 0, st>>>(a, steps);
+    });
+  }
+  qk_gain_grad_kernel<<<(2 * a.hd + 15) / 16, 1024, 0, st>>>(a.part, grid, a.hd, dgq, dgk);
 }
 
 template <typename T>
@@ -1020,7 +1071,7 @@ alr_status layer_forward(alr_ctx* ctx, int l, int M, bool decode, int s, float* 
     a.gk = lw + L.l_knorm;
     a.pos = rr.pos;
     a.pos_add = rr.pos_add;
-    launch_qk<T>(a, st);
+    launch_qk<T>(ctx, a, st);
     ALR_LAUNCHED(ctx, "q/k norm");
   }
 
@@ -2321,9 +2372,9 @@ alr_status alr_qk_norm_rope(alr_ctx* ctx, int32_t n, int32_t q_heads, int32_t k_
   a.pos = positions;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (ctx->cfg.dtype == ALR_BF16)
-    launch_qk<bf16>(a, s);
+    launch_qk<bf16>(ctx, a, s);
   else
-    launch_qk<float>(a, s);
+    launch_qk<float>(ctx, a, s);
   ALR_LAUNCHED(ctx, "q/k norm");
   return ALR_OK;
 }
