@@ -96,7 +96,7 @@ __global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
     if (a.up) inv_w *= a.up[0];
   }
   for (long r = blockIdx.x; r < a.n; r += gridDim.x) {
-    const RowChunks<T> row(static_cast<const T*>(a.z) + r * a.z_rs, a.V);
+    RowChunks<T> row(static_cast<const T*>(a.z) + r * a.z_rs, a.V);
     const int cpw = (row.nch + THREADS - 1) / THREADS;
     T* dz = GRAD ? static_cast<T*>(a.dz) + r * a.dz_rs : nullptr;
     const bool vec =
@@ -113,6 +113,7 @@ __global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
       }
       continue;
     }
+    row.edges();
     // the label; an id outside the vocabulary is passed over with its probability
     int id[DISTILL_K];
     float pi[DISTILL_K], zj[DISTILL_K];
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
       const int c = (wave * cpw + i) * 64 + lane;
       if (c >= row.nch) break;
       float v[EPC];
-      unpack<T>(row.load(c), v);
+      unpack<T>(row.whole(c, row.load(c)), v);
       if (hit >> (i & 31) & 1)
 #pragma unroll
         for (int k = 0; k < EPC; ++k)
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
         const int c = (wave * cpw + i) * 64 + lane;
         if (c >= row.nch) break;
         float v[EPC];
-        unpack<T>(row.load(c), v);
+        unpack<T>(row.whole(c, row.load(c)), v);
         float g[EPC];
 #pragma unroll
         for (int k = 0; k < EPC; ++k) g[k] = bt * fast_exp2((v[k] - ref_t) * LOG2E);

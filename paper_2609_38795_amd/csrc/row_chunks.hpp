@@ -9,39 +9,53 @@ namespace alr {
 constexpr float LOG2E = 1.44269504088896340736f;
 
 // One row of V values of T, whose first value may sit anywhere within a 16-byte line: chunk c
-// holds the values [c * EPC - mis, c * EPC - mis + EPC) that exist.  Chunks that lie inside the
-// row are moved by one 16-byte access, the one or two at its ends value by value, so nothing
-// outside the row is touched.
+// holds the values [c * EPC - mis, c * EPC - mis + EPC) that exist, and -inf in the places of the others.
+// Chunks [cf, cl) lie inside the row and are moved by one 16-byte access; the one or two at its ends are read value
+// by value, once per row (edges()), so nothing outside the row is touched.
 template <typename T>
 struct RowChunks {
   static constexpr int EPC = 16 / (int)sizeof(T);
+  static constexpr uint32_t NEG = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;  // -inf
   const T* p;
-  int V, mis, nch;
+  int V, mis, nch, cf, cl;
+  u32x4 e0, e1;  // the chunks at the ends
 
   __device__ __forceinline__ RowChunks(const T* row, int V_) : p(row), V(V_) {
     mis = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
     nch = (V + mis + EPC - 1) / EPC;
+    cf = mis ? 1 : 0;
+    cl = (V + mis) / EPC;
+  }
+  __device__ __forceinline__ void edges() {
+    e0 = e1 = u32x4{NEG, NEG, NEG, NEG};
+    if (cf) e0 = edge(0);
+    if (cl < nch) e1 = edge(nch - 1);
   }
   __device__ __forceinline__ int first(int c) const { return c * EPC - mis; }
-  __device__ __forceinline__ bool inside(int c) const {
-    const int e0 = first(c);
-    return e0 >= 0 && e0 + EPC <= V;
-  }
-  // chunk c; -inf where it reaches past the row (all of it for c >= nch)
+  __device__ __forceinline__ bool inside(int c) const { return c >= cf && c < cl; }
+  // What load() gives is chunk c where that lies inside the row; whole() makes it chunk c in any
+  // case.  In two steps, so that several loads can be under way before the first is looked at.
   __device__ __forceinline__ u32x4 load(int c) const {
-    if (inside(c)) return *reinterpret_cast<const u32x4*>(p + first(c));
-    return edge(c);
+    if (cf >= cl) return u32x4{NEG, NEG, NEG, NEG};
+    return *reinterpret_cast<const u32x4*>(p + first(min(max(c, cf), cl - 1)));
   }
-  __device__ u32x4 edge(int c) const {
+  __device__ __forceinline__ u32x4 whole(int c, u32x4 w) const {
+    if (!inside(c)) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = c == 0 && cf ? e0[k] : c == nch - 1 ? e1[k] : NEG;
+    }
+    return w;
+  }
+  __device__ __forceinline__ u32x4 edge(int c) const {
     u32x4 w;
-    const int e0 = first(c);
+    const int e = first(c);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if constexpr (sizeof(T) == 4) {
-        const int e = e0 + k;
-        w[k] = e >= 0 && e < V ? __float_as_uint(p[e]) : 0xFF800000u;
+        const int a = e + k;
+        w[k] = a >= 0 && a < V ? __float_as_uint(p[a]) : NEG;
       } else {
-        const int a = e0 + 2 * k, b = a + 1;
+        const int a = e + 2 * k, b = a + 1;
         const uint32_t lo = a >= 0 && a < V ? (uint32_t)p[a] : 0xFF80u;
         const uint32_t hi = b >= 0 && b < V ? (uint32_t)p[b] : 0xFF80u;
         w[k] = lo | hi << 16;

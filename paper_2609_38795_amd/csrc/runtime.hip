@@ -1241,7 +1241,7 @@ template <typename T>
 void launch_sample(const SampleArgs& a, hipStream_t st) {
   const unsigned grid = (unsigned)std::min<long>(a.n, 1 << 20);
   if (a.V > 8192)
-    sample_kernel<T, 1024><<<grid, 1024, 0, st>>>(a);
+    sample_kernel<T, 512><<<grid, 512, 0, st>>>(a);
   else
     sample_kernel<T, 256><<<grid, 256, 0, st>>>(a);
 }

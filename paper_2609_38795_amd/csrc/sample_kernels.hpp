@@ -10,9 +10,9 @@
 // the weight, falls into, histograms over the bits of the logits narrow it to one value, and a scan
 // over the ids settles the ties.
 //
-// Weights are whole numbers of 2^-shift (shift >= 43, from 64-bit exponentials), so every sum is exact
+// Weights are whole numbers of 2^-shift (shift >= 43), from 64-bit exponentials, so every sum is exact
 // and does not depend on the order in which it is formed: what a row gives depends on its own values
-// alone, and is what 64-bit arithmetic gives up to 2^-shift of the largest weight.
+// alone, and is what 64-bit arithmetic gives up to 2^-43 of a weight and of the largest one.
 #pragma once
 
 #include "row_chunks.hpp"
@@ -40,32 +40,41 @@ struct SampleArgs {
 
 typedef unsigned long long u64;
 
-constexpr int SAMPLE_BINS = 2048;
-constexpr int SAMPLE_GROUPS = 4;  // parts of a wave's run whose weights are summed apart
+constexpr int SAMPLE_BINS = 1024, SAMPLE_BITS = 10;
+constexpr int SAMPLE_GROUPS = 8;    // parts of a row whose weights are summed apart for the draw
+constexpr int SAMPLE_STEPS = 16;    // chunks of a thread within one such part, at most
+constexpr int SAMPLE_LIST = 4096;   // logits that may be set aside
 
-__device__ __forceinline__ u64 shfl_xor_u64(u64 v, int o) {
-  const uint32_t lo = __shfl_xor((uint32_t)v, o), hi = __shfl_xor((uint32_t)(v >> 32), o);
-  return (u64)hi << 32 | lo;
+// v of the lane that a DPP control names, 0 where there is none or the row is masked off
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_0(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
 }
-__device__ __forceinline__ u64 shfl_up_u64(u64 v, int o) {
-  const uint32_t lo = __shfl_up((uint32_t)v, o), hi = __shfl_up((uint32_t)(v >> 32), o);
-  return (u64)hi << 32 | lo;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 dpp_or_0(u64 v) {
+  return (u64)dpp_or_0<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | dpp_or_0<CTRL, ROWS>((uint32_t)v);
 }
-__device__ __forceinline__ u64 wave_sum_u64(u64 v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += shfl_xor_u64(v, o);
+// Sum over this lane and those before it: within rows of 16 lanes, then rows 1 and 3 take the last lane
+// of the row before them, then rows 2 and 3 lane 31.  All lanes must be active.
+template <typename N>
+__device__ __forceinline__ N wave_upto(N v) {
+  v += dpp_or_0<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
+  v += dpp_or_0<0x112, 0xF>(v);
+  v += dpp_or_0<0x114, 0xF>(v);
+  v += dpp_or_0<0x118, 0xF>(v);
+  v += dpp_or_0<0x142, 0xA>(v);  // row_bcast 15
+  v += dpp_or_0<0x143, 0xC>(v);  // row_bcast 31
   return v;
 }
-// sum over the lanes before this one
-__device__ __forceinline__ u64 wave_before_u64(u64 v) {
-  u64 t = v;
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const u64 x = shfl_up_u64(t, o);
-    if (lane >= o) t += x;
-  }
-  return t - v;
+__device__ __forceinline__ uint32_t last_lane(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ u64 last_lane(u64 v) {
+  return (u64)last_lane((uint32_t)(v >> 32)) << 32 | last_lane((uint32_t)v);
+}
+template <typename N>
+__device__ __forceinline__ N wave_total(N v) {
+  return last_lane(wave_upto(v));
 }
 
 // Unsigned order of the floats' order; -0 as +0.
@@ -103,38 +112,67 @@ __device__ __forceinline__ double exp2_scaled(double y, int shift) {
   return __builtin_ldexp(p, n + shift);
 }
 
-// The weight of a logit, in units of 2^-shift of the largest one's.
+// The weight of a logit, in units of 2^-shift of the largest one's: with y = (z - m) 32 log2(e) / T =
+// k + f, |f| <= 1/2, the weight is 2^(k / 32) times a polynomial of 2^(f / 32).  2^((k mod 32) / 32) comes from a
+// table, the rest of k is added to its exponent, and adding 2^52 rounds to whole units.  The polynomial is
+// the series of exp up to the 5th power with that power replaced by the lower ones that differ least
+// from it on [-1/2, 1/2] (Chebyshev): 2^-43 of the weight.
 struct Weigher {
-  double m, c;  // the row's largest logit; log2(e) / T
+  double m, c, floor;  // the row's largest logit; 32 log2(e) / T; the lowest z - m: weights below are 0
   int shift;
-  __device__ __forceinline__ double of(float z) const {
-    return exp2_scaled(((double)z - m) * c, shift);
+  const double* tab;   // 2^(shift + j / 32), j < 32
+  __device__ __forceinline__ void set(float m_, float temp, int shift_, const double* tab_) {
+    m = (double)m_;
+    c = fmax(32.0 * 1.4426950408889634074 / (double)temp, 1e-300);
+    floor = -28800.0 / c;
+    shift = shift_;
+    tab = tab_;
   }
-  __device__ __forceinline__ u64 units(float z) const {  // of() <= 2^51: rounded by adding 2^52
-    constexpr double ONE52 = 4503599627370496.0;
-    return (u64)__double_as_longlong(of(z) + ONE52) & ((1ull << 52) - 1);
+  __device__ __forceinline__ u64 units(float z) const {
+    constexpr double MAGIC = 6755399441055744.0, ONE52 = 4503599627370496.0;
+    constexpr double L = 0.693147180559945309417232 / 32, A2 = 0.25;  // A2: (half width)^2
+    constexpr double c5 = L * L * L * L * L / 120;
+    constexpr double c1 = L - c5 * A2 * A2 * 5 / 16, c2 = L * L / 2, c3 = L * L * L / 6 + c5 * A2 * 5 / 4,
+                     c4 = L * L * L * L / 24;
+    const double d = fmax((double)z - m, floor);
+    const double t = fma(d, c, MAGIC);
+    const double f = fma(d, c, -(t - MAGIC));
+    const uint32_t k = (uint32_t)__double_as_longlong(t);
+    const u64 w = (u64)__double_as_longlong(tab[k & 31]) + ((u64)((k & ~31u) << 15) << 32);
+    double p = fma(f, c4, c3);
+    p = fma(f, p, c2);
+    p = fma(f, p, c1);
+    p = fma(f, p, 1.0);
+    return (u64)__double_as_longlong(fma(p, __longlong_as_double((long long)w), ONE52)) & ((1ull << 52) - 1);
   }
+  __device__ __forceinline__ double log2_of(float z) const { return ((double)z - m) * c * (1.0 / 32); }
 };
 
 struct SampleShared {
-  uint32_t cnt[2][SAMPLE_BINS];  // of the first level, of the narrowing ones
+  double tab[32];
+  uint32_t cnt[2][SAMPLE_BINS];  // of the first level over a row, of the narrowing ones
   u64 mass[2][SAMPLE_BINS];
-  u64 scan_c[16], scan_m[16];
-  u64 group[16][SAMPLE_GROUPS];
-  float fred[16];
+  f32x2 list[SAMPLE_LIST];       // (logit, id) of the logits set aside, a run of it per wave
+  uint32_t scan_c[16], few_n;
+  u64 scan_m[16];
+  u64 part[SAMPLE_STEPS][16];
+  uint32_t few_key[64];
+  u64 few_w[64];
+  float fred[4][16];
   uint32_t ured[2][16];
   int bin;
-  u64 above_c, above_m;
+  uint32_t above_c;
+  u64 above_m;
 };
 
 template <int NW>
 __device__ __forceinline__ float block_max_f(float v, SampleShared& sh) {
   v = wave_max(v);
-  if ((threadIdx.x & 63) == 0) sh.fred[threadIdx.x >> 6] = v;
+  if ((threadIdx.x & 63) == 0) sh.fred[0][threadIdx.x >> 6] = v;
   __syncthreads();
-  float t = sh.fred[0];
+  float t = sh.fred[0][0];
 #pragma unroll
-  for (int i = 1; i < NW; ++i) t = fmaxf(t, sh.fred[i]);
+  for (int i = 1; i < NW; ++i) t = fmaxf(t, sh.fred[0][i]);
   __syncthreads();
   return t;
 }
@@ -160,8 +198,29 @@ __device__ __forceinline__ void block_range(uint32_t& lo, uint32_t& hi, SampleSh
   __syncthreads();
 }
 
+// a count and a sum of weights over the workgroup
+template <int NW>
+__device__ __forceinline__ void block_sums(uint32_t& c, u64& m, SampleShared& sh) {
+  c = wave_total(c);
+  m = wave_total(m);
+  if ((threadIdx.x & 63) == 0) {
+    sh.scan_c[threadIdx.x >> 6] = c;
+    sh.scan_m[threadIdx.x >> 6] = m;
+  }
+  __syncthreads();
+  c = 0;
+  m = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    c += sh.scan_c[i];
+    m += sh.scan_m[i];
+  }
+  __syncthreads();
+}
+
 template <int THREADS>
 __device__ __forceinline__ void clear_bins(SampleShared& sh, int level) {
+#pragma unroll
   for (int b = threadIdx.x; b < SAMPLE_BINS; b += THREADS) {
     sh.cnt[level][b] = 0;
     sh.mass[level][b] = 0;
@@ -169,33 +228,33 @@ __device__ __forceinline__ void clear_bins(SampleShared& sh, int level) {
   __syncthreads();
 }
 
-// What is looked for in the bins of a level: the bin with the token of rank `count`
-// (counting from 1), or the one in which the weight of the ranking's prefix reaches `mass`, or, before the
-// whole weight is known, `share` of the weight that the bins hold.
+// What is looked for among ranked values: the `want`-th (counting from 1), or, by_mass, the one with which
+// the weights added up reach `want` >= 1.
 struct Aim {
   bool by_mass;
-  u64 count, mass;
-  double share;  // > 0: mass = share of the total, rounded up
+  u64 want;
 };
 
-// Finds the bin; above_c and above_m come in as what ranks before the level's bins and go out as
-// what ranks before the bin.  Returns -1 where the level's tokens are fewer than `count`.
-// Everything else that needs the level's total weight gets it in `total`.
-template <int THREADS>
-__device__ __forceinline__ int find_bin(SampleShared& sh, int level, Aim& aim, u64& above_c,
-                                        u64& above_m, u64& total) {
+// Finds the aim's bin; above_c and above_m come in as what lies before the level's bins and go out as
+// what lies before the bin.  Returns -1 where the bins do not reach it.  mass_of(total weight of
+// the bins) may still set the aim (a share of a whole that only the bins know).
+template <int THREADS, typename F>
+__device__ __forceinline__ int find_bin(SampleShared& sh, int level, Aim& aim, uint32_t& above_c,
+                                        u64& above_m, F mass_of) {
   constexpr int NW = THREADS / 64, PER = SAMPLE_BINS / THREADS;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b0 = threadIdx.x * PER;
-  u64 c = 0, m = 0;
-#pragma unroll 4
+  uint32_t c = 0;
+  u64 m = 0;
+#pragma unroll
   for (int i = 0; i < PER; ++i) {
     c += sh.cnt[level][b0 + i];
     m += sh.mass[level][b0 + i];
   }
-  u64 c_before = wave_before_u64(c), m_before = wave_before_u64(m);
+  uint32_t c_upto = wave_upto(c);
+  u64 m_upto = wave_upto(m);
   if (lane == 63) {
-    sh.scan_c[wave] = c_before + c;
-    sh.scan_m[wave] = m_before + m;
+    sh.scan_c[wave] = c_upto;
+    sh.scan_m[wave] = m_upto;
   }
   if (threadIdx.x == 0) sh.bin = -1;
   __syncthreads();
@@ -203,25 +262,19 @@ __device__ __forceinline__ int find_bin(SampleShared& sh, int level, Aim& aim, u
 #pragma unroll
   for (int i = 0; i < NW; ++i) {
     if (i < wave) {
-      c_before += sh.scan_c[i];
-      m_before += sh.scan_m[i];
+      c_upto += sh.scan_c[i];
+      m_upto += sh.scan_m[i];
     }
     all += sh.scan_m[i];
   }
-  total = all;
-  if (aim.by_mass && aim.share > 0.0) {
-    aim.mass = (u64)ceil(aim.share * (double)all);
-    aim.share = 0.0;
-  }
-  if (aim.by_mass && aim.mass < 1) aim.mass = 1;
-  c_before += above_c;
-  m_before += above_m;
-  const u64 want = aim.by_mass ? aim.mass : aim.count;
+  mass_of(all);
+  uint32_t c_before = above_c + c_upto - c;
+  u64 m_before = above_m + m_upto - m;
   u64 at = aim.by_mass ? m_before : c_before;
-  if (at < want && at + (aim.by_mass ? m : c) >= want) {
+  if (at < aim.want && at + (aim.by_mass ? m : c) >= aim.want) {
     for (int i = 0; i < PER; ++i) {
       const u64 x = aim.by_mass ? sh.mass[level][b0 + i] : sh.cnt[level][b0 + i];
-      if (at + x >= want) {
+      if (at + x >= aim.want) {
         sh.bin = b0 + i;
         sh.above_c = c_before;
         sh.above_m = m_before;
@@ -238,8 +291,82 @@ __device__ __forceinline__ int find_bin(SampleShared& sh, int level, Aim& aim, u
     above_c = sh.above_c;
     above_m = sh.above_m;
   }
-  __syncthreads();  // the level's bins and sh.bin may be written again
+  __syncthreads();  // sh.bin may be written again
   return bin;
+}
+
+// Among the values that `each` visits (f(key, logit) per value of interest), those with keys within [lo, hi]:
+// the key that the aim falls on, keys counted from the largest down, or, `up`, from the smallest up;
+// above_c and above_m come in as what lies before hi (lo) and end as what lies before that key.  A level
+// of bins over the keys' range leaves few values as a rule, which are ranked against each other; else another
+// level splits the bin.  False where the values do not reach the aim.
+template <int THREADS, typename E>
+__device__ __forceinline__ bool pick(SampleShared& sh, const Weigher& wt, bool up, Aim aim, uint32_t lo,
+                                     uint32_t hi, uint32_t& above_c, u64& above_m, uint32_t& found,
+                                     E each) {
+  while (true) {
+    const uint32_t range = hi - lo;
+    const int shift = range ? max(0, 32 - SAMPLE_BITS - (int)__clz(range)) : 0;  // range >> shift: a bin
+    if (threadIdx.x == 0) sh.few_n = 0;
+    clear_bins<THREADS>(sh, 1);
+    each([&](uint32_t key, float z) {
+      if (key >= lo && key <= hi) {
+        const uint32_t b = (up ? key - lo : hi - key) >> shift;
+        atomicAdd(&sh.cnt[1][b], 1u);
+        atomicAdd(&sh.mass[1][b], wt.units(z));
+      }
+    });
+    __syncthreads();
+    const int b = find_bin<THREADS>(sh, 1, aim, above_c, above_m, [](u64) {});
+    if (b < 0) return false;
+    const uint32_t width = (1u << shift) - 1, n = sh.cnt[1][b];
+    if (up) {
+      lo += (uint32_t)b << shift;
+      hi = min(hi, lo + min(0xFFFFFFFFu - lo, width));
+    } else {
+      hi -= (uint32_t)b << shift;
+      lo = max(lo, hi - min(hi, width));
+    }
+    __syncthreads();  // cnt may be cleared again
+    if (lo == hi) {
+      found = lo;
+      return true;
+    }
+    if (n > 64) continue;
+    each([&](uint32_t key, float z) {
+      if (key >= lo && key <= hi) {
+        const uint32_t at = atomicAdd(&sh.few_n, 1u);
+        sh.few_key[at] = key;
+        sh.few_w[at] = wt.units(z);
+      }
+    });
+    __syncthreads();
+    // every wave ranks them: lane l's value against all
+    const int lane = threadIdx.x & 63;
+    const uint32_t mine = sh.few_key[min((uint32_t)lane, n - 1)];
+    uint32_t c = 0, c_own = 0;
+    u64 m = 0, m_own = 0;
+    for (uint32_t i = 0; i < n; ++i) {
+      const uint32_t key = sh.few_key[i];
+      const u64 w = sh.few_w[i];
+      if (key == mine) {
+        ++c_own;
+        m_own += w;
+      } else if (up ? key < mine : key > mine) {
+        ++c;
+        m += w;
+      }
+    }
+    const u64 at = aim.by_mass ? above_m + m : above_c + c;
+    const bool hit = (uint32_t)lane < n && at < aim.want && at + (aim.by_mass ? m_own : c_own) >= aim.want;
+    const int src = __ffsll((unsigned long long)__ballot(hit)) - 1;
+    found = (uint32_t)__builtin_amdgcn_readlane((int)mine, src);
+    above_c += (uint32_t)__builtin_amdgcn_readlane((int)c, src);
+    above_m += (u64)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(m >> 32), src) << 32 |
+               (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)m, src);
+    __syncthreads();
+    return true;
+  }
 }
 
 // Where the kept prefix ends: logits above `z`, and of those equal to z the first `ties` ids.
@@ -247,27 +374,66 @@ struct Cut {
   float z;
   u64 ties;
 };
+constexpr u64 ALL_TIES = ~0ull;
 
+// One workgroup per row.  What bounds a row is its reads (the first from HBM, a second, where there is one,
+// mostly from the last-level cache) and, where every weight is needed, the 64-bit exponentials, about 15
+// operations each.
+//
+// Pass 1 takes the maximum, and the maxima of a thousand parts of the row: most of their spread lies
+// above the few thousandths of the row that limits usually keep.  Pass 2 sets the logits above a line drawn from
+// them aside (in LDS) and, for a top_p of the whole row, forms the histogram of the weights over (max - z) / T.
+// Limits that fall within the list are settled there, and so is the draw.  Others (a nucleus of a flat
+// distribution, a k of thousands) are narrowed to a bin of the histogram, the bin's logits are set aside
+// instead, and the draw reads the row again.
+//
+// Rows of different limits cost differently and limits tend to repeat, so a group of eight rows is dealt
+// to the eight XCDs in a rotating order.
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
-  constexpr int NW = THREADS / 64, EPC = RowChunks<T>::EPC;
+__global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleArgs a) {
+  constexpr int NW = THREADS / 64, EPC = RowChunks<T>::EPC, RUN = SAMPLE_LIST / NW;
   static_assert(SAMPLE_BINS % THREADS == 0 && NW <= 16, "bins per thread");
   __shared__ SampleShared sh;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (long r = blockIdx.x; r < a.n; r += gridDim.x) {
+  if (threadIdx.x < 32) sh.tab[threadIdx.x] = exp2((double)threadIdx.x / 32 + a.shift);
+  for (long b = blockIdx.x; b < a.n; b += gridDim.x) {
+    const long r = (b | 7) < a.n ? (b & ~7L) | ((b + (b >> 3)) & 7) : b;
     const long idx = a.perm ? (long)a.perm[r] : r, o = idx * a.block + a.s;
-    const RowChunks<T> row(static_cast<const T*>(a.z) + (a.z_perm ? idx : r) * a.z_rs, a.V);
-    const int cpw = (row.nch + THREADS - 1) / THREADS;
-    // f(value, id) over this wave's run of the row, chunks [i0, i1) of it
-    auto each = [&](int i0, int i1, auto f) {
-      for (int i = i0; i < i1; ++i) {
-        const int c = (wave * cpw + i) * 64 + lane;
-        if (c >= row.nch) break;
-        float v[EPC];
-        unpack<T>(row.load(c), v);
+    RowChunks<T> row(static_cast<const T*>(a.z) + (a.z_perm ? idx : r) * a.z_rs, a.V);
+    row.edges();
+    // thread t's chunk i is i * THREADS + t: ids rise with i, then with the thread
+    const int cpt = (row.nch + THREADS - 1) / THREADS;
+    // f(i, logits, first id) for chunks [i0, i1) of the thread, U loads in flight
+    auto chunks = [&](auto u_, int i0, int i1, auto f) {
+      constexpr int U = decltype(u_)::value;
+#pragma unroll 1
+      for (int i = i0; i < i1; i += U) {
+        u32x4 w[U];
 #pragma unroll
-        for (int k = 0; k < EPC; ++k) f(v[k], row.first(c) + k);
+        for (int u = 0; u < U; ++u) w[u] = row.load((i + u) * THREADS + (int)threadIdx.x);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (i + u >= i1) break;
+          const int c = (i + u) * THREADS + (int)threadIdx.x;
+          float v[EPC];
+          unpack<T>(row.whole(c, w[u]), v);
+          f(i + u, v, row.first(c));
+        }
       }
+    };
+    using light = std::integral_constant<int, 8>;
+    using heavy = std::integral_constant<int, 2>;  // passes that weigh every logit
+    using single = std::integral_constant<int, 1>;
+    // f(logit, id) over the row.  Weights take many registers: two at a time are enough to fill the
+    // pipeline with four waves per SIMD.
+    auto each = [&](auto u_, auto f) {
+      chunks(u_, 0, cpt, [&](int, const float(&v)[EPC], int e0) {
+#pragma unroll
+        for (int k = 0; k < EPC; ++k) {
+          f(v[k], e0 + k);
+          if (decltype(u_)::value <= 2 && (k & 1)) __builtin_amdgcn_sched_barrier(0);
+        }
+      });
     };
     auto emit = [&](int tok, float lp) {
       a.tokens[o] = tok;
@@ -278,9 +444,13 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
       }
     };
 
-    float m = -INFINITY;
-    each(0, cpw, [&](float z, int) { m = fmaxf(m, z); });
-    m = block_max_f<NW>(m, sh);
+    // pass 1
+    float part[2] = {-INFINITY, -INFINITY};
+    chunks(light{}, 0, cpt, [&](int i, const float(&v)[EPC], int) {
+#pragma unroll
+      for (int k = 0; k < EPC; ++k) part[i & 1] = fmaxf(part[i & 1], v[k]);
+    });
+    const float m = block_max_f<NW>(fmaxf(part[0], part[1]), sh);
     if (m == -INFINITY) {  // nothing to draw
       if (threadIdx.x == 0) emit(-1, -INFINITY);
       continue;
@@ -288,194 +458,341 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     const float temp = a.temperature ? a.temperature[idx] : 1.f;
     if (!(temp > 0.f) || m == INFINITY) {  // greedy: the lowest id at the maximum
       uint32_t lo = 0xFFFFFFFFu, hi = 0;
-      each(0, cpw, [&](float z, int e) {
+      each(light{}, [&](float z, int e) {
         if (z == m) lo = min(lo, (uint32_t)e);
       });
       block_range<NW>(lo, hi, sh);
       if (threadIdx.x == 0) emit((int)lo, 0.f);
       continue;
     }
-    const Weigher wt{(double)m, 1.4426950408889634074 / (double)temp, a.shift};
-    const int k = a.top_k ? a.top_k[idx] : 0;
-    const float p = a.top_p ? a.top_p[idx] : 1.f;
-    const bool by_k = k > 0 && k < a.V, by_p = p < 1.f;
-    Cut cut = {-INFINITY, 0};
-    if (by_k || by_p) {
-      // level 0: bins of 1/64 in (max - z) / T, the last one for all that lies below
-      const float cs = fminf(64.f / temp, 1e30f);
-      auto bin0 = [&](float z) { return (int)fminf((m - z) * cs, (float)(SAMPLE_BINS - 1)); };
-      clear_bins<THREADS>(sh, 0);
-      each(0, cpw, [&](float z, int) {
-        if (z == z && z != -INFINITY) {
-          const int b = bin0(z);
-          if (by_k) atomicAdd(&sh.cnt[0][b], 1u);
-          if (by_p) atomicAdd(&sh.mass[0][b], wt.units(z));
-        }
-      });
-      __syncthreads();
-      // narrows a bin of level 0 to one logit
-      auto narrow = [&](int bin, Aim aim, u64& above_c, u64& above_m) {
-        uint32_t lo = 0xFFFFFFFFu, hi = 0;
-        each(0, cpw, [&](float z, int) {
-          if (z == z && z != -INFINITY && bin0(z) == bin) {
-            const uint32_t key = order_key(z);
-            lo = min(lo, key);
-            hi = max(hi, key);
-          }
-        });
-        block_range<NW>(lo, hi, sh);
-        while (lo < hi) {
-          const int shift = max(0, 21 - (int)__clz(hi - lo));  // (hi - lo) >> shift < 2048
-          clear_bins<THREADS>(sh, 1);
-          each(0, cpw, [&](float z, int) {
-            const uint32_t key = order_key(z);
-            if (z == z && key >= lo && key <= hi) {
-              const uint32_t b = (hi - key) >> shift;
-              if (by_k) atomicAdd(&sh.cnt[1][b], 1u);
-              if (by_p) atomicAdd(&sh.mass[1][b], wt.units(z));
-            }
-          });
-          __syncthreads();
-          u64 all;
-          const int b = find_bin<THREADS>(sh, 1, aim, above_c, above_m, all);
-          if (b < 0) break;  // not reached: the level holds what the one above it counted
-          hi -= (uint32_t)b << shift;
-          lo = max(lo, hi - min(hi, (1u << shift) - 1));
-        }
-        return key_value(hi);
-      };
-      u64 total, mass_k = 0;
-      if (by_k) {
-        u64 above_c = 0, above_m = 0;
-        Aim aim{false, (u64)k, 0, 0.0};
-        const int bin = find_bin<THREADS>(sh, 0, aim, above_c, above_m, total);
-        if (bin >= 0) {
-          cut.z = narrow(bin, aim, above_c, above_m);
-          cut.ties = (u64)k - above_c;
-          mass_k = above_m + cut.ties * wt.units(cut.z);
-        } else {
-          mass_k = total;  // fewer than k tokens can be drawn
-        }
-      }
-      if (by_p) {
-        u64 above_c = 0, above_m = 0;
-        Aim aim{true, 0, 0, 0.0};
-        if (by_k)
-          aim.mass = p > 0.f ? (u64)ceil((double)p * (double)mass_k) : 0;
-        else
-          aim.share = p > 0.f ? (double)p : 0.0;
-        const int bin = find_bin<THREADS>(sh, 0, aim, above_c, above_m, total);
-        if (bin >= 0) {
-          const float z = narrow(bin, aim, above_c, above_m);
-          const u64 need = aim.mass - above_m, one = max(wt.units(z), 1ull);
-          const u64 ties = (need + one - 1) / one;
-          if (z > cut.z) {
-            cut = {z, ties};
-          } else if (z == cut.z) {
-            cut.ties = min(cut.ties, ties);
-          }
-        }
-      }
-    }
-    const float mp = a.min_p ? a.min_p[idx] : 0.f;
+    Weigher wt;
+    wt.set(m, temp, a.shift, sh.tab);
+    const uint32_t k = a.top_k ? (uint32_t)max(a.top_k[idx], 0) : 0;
+    const float p = a.top_p ? a.top_p[idx] : 1.f, mp = a.min_p ? a.min_p[idx] : 0.f;
+    const bool by_k = k > 0 && k < (uint32_t)a.V, by_p = p < 1.f;
+    const double share = fmax((double)p, 0.0);
+    const double u = fmin(fmax((double)a.uniform[o], 0.0), 1.0 - 0x1p-24);
+    auto share_of = [&](u64 w) { return max((u64)ceil(share * (double)w), 1ull); };
+    auto emit_drawn = [&](float z, int e, u64 total) {
+      emit(e, (float)((wt.log2_of(z) + wt.shift - log2((double)total)) * 0.69314718055994530942));
+    };
+
+    Cut cut = {-INFINITY, ALL_TIES};
     if (mp > 0.f) {
       // the lowest float whose weight is at least min_p: near m + T ln p, then step by step
       const double want = fmin((double)mp, 1.0);
-      auto keeps = [&](float z) { return exp2_scaled(((double)z - wt.m) * wt.c, 0) >= want; };
-      uint32_t key = order_key((float)fmax(wt.m + log2(want) / wt.c, -3.4e38));
+      auto keeps = [&](float z) { return exp2(wt.log2_of(z)) >= want; };
       const uint32_t top = order_key(m);
-      key = min(key, top);
+      uint32_t key = min(order_key((float)fmax(wt.m + 32 * log2(want) / wt.c, -3.4e38)), top);
       for (int i = 0; i < 64 && key < top && !keeps(key_value(key)); ++i) ++key;
       for (int i = 0; i < 64 && key > 0x00800000u && keeps(key_value(key - 1)); ++i) --key;
-      const float z = key_value(key);
-      if (z > cut.z) cut = {z, ~0ull};
+      cut.z = key_value(key);
     }
-    // ids up to id_lim are kept at the cut itself
-    uint32_t id_lim = 0xFFFFFFFFu;
-    if (cut.z != -INFINITY && cut.ties != ~0ull) {
-      u64 here = 0;
-      each(0, cpw, [&](float z, int) { here += z == cut.z ? 1 : 0; });
-      const u64 mine = wave_sum_u64(here);
+
+    // pass 2: the list of logits >= line, each wave's share in its own run
+    uint32_t mine = 0, n_list = 0;  // entries of this wave, of all
+    auto set_aside = [&](float z, int e, bool in) {
+      const u64 bits = __ballot(in);
+      if (bits == 0) return;
+      const uint32_t at = mine + __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32),
+                                                          __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
+      if (in && at < RUN) sh.list[wave * RUN + at] = f32x2{z, __int_as_float(e)};
+      mine += (uint32_t)__popcll(bits);
+    };
+    auto each_listed = [&](auto f) {
+      for (uint32_t i = lane; i < mine; i += 64) {
+        const f32x2 x = sh.list[wave * RUN + i];
+        f(x[0], __float_as_int(x[1]));
+      }
+    };
+    auto list_closed = [&]() {  // whether every wave's share fitted its run
       if (lane == 0) sh.scan_c[wave] = mine;
-      if (threadIdx.x == 0) sh.bin = -1;
       __syncthreads();
-      u64 before = 0, all = 0;
+      bool fits = true;
+      n_list = 0;
 #pragma unroll
       for (int i = 0; i < NW; ++i) {
-        if (i < wave) before += sh.scan_c[i];
-        all += sh.scan_c[i];
+        fits &= sh.scan_c[i] <= RUN;
+        n_list += sh.scan_c[i];
       }
-      if (cut.ties < all && before < cut.ties && before + mine >= cut.ties) {
-        // the wave that holds the last tie kept
-        for (int i = 0; i < cpw; ++i) {
-          u64 x = 0;
-          each(i, i + 1, [&](float z, int) { x += z == cut.z ? 1 : 0; });
-          const u64 sum = wave_sum_u64(x);
-          if (before + sum >= cut.ties) {
-            u64 at = before + wave_before_u64(x);
-            each(i, i + 1, [&](float z, int e) {
-              if (z == cut.z && ++at == cut.ties) sh.bin = e;
-            });
-            break;
+      __syncthreads();
+      return fits;
+    };
+    auto real = [](float z) { return z > -INFINITY; };  // neither nan nor -inf
+    // bins of 1/32 in (max - z) / T, the last one for all that lies below
+    const float cs = fminf(32.f / temp, 1e30f);
+    auto bin0 = [&](float z) { return (int)fminf((m - z) * cs, (float)(SAMPLE_BINS - 1)); };
+    const bool limits = by_k || by_p || mp > 0.f;
+    // the line: 1.5 standard deviations below the mean of the parts' maxima (an estimate, any line is
+    // right), or where min_p ends if nothing below counts
+    float line = -INFINITY;
+    if (limits && a.V > SAMPLE_LIST / 2) {
+      float c = 0.f, s1 = 0.f, s2 = 0.f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (part[h] != -INFINITY) {
+          const float d = m - part[h];
+          c += 1.f;
+          s1 += d;
+          s2 += d * d;
+        }
+      c = wave_sum(c);
+      s1 = wave_sum(s1);
+      s2 = wave_sum(s2);
+      if (lane == 0) {
+        sh.fred[1][wave] = c;
+        sh.fred[2][wave] = s1;
+        sh.fred[3][wave] = s2;
+      }
+      __syncthreads();
+      c = s1 = s2 = 0.f;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) {
+        c += sh.fred[1][i];
+        s1 += sh.fred[2][i];
+        s2 += sh.fred[3][i];
+      }
+      __syncthreads();
+      const float mean = s1 / c;
+      line = m - (mean + 1.5f * sqrtf(fmaxf(s2 / c - mean * mean, 0.f)));
+    }
+    const bool below_counts = by_k && by_p;  // top_p's share is of the first k, min_p or not
+    const bool at_min_p = limits && !below_counts && cut.z >= line;
+    if (at_min_p) line = cut.z;
+    const bool all = line == -INFINITY || at_min_p;  // what is not listed is not kept
+    // listed: every logit that may be kept is in the list (and the limits are settled there).  With a
+    // top_p of the whole row, or where the list turns out too short, the first level of bins over the row.
+    bool listed = false, binned = by_p && !by_k;
+    uint32_t key_lo = order_key(line), key_hi = order_key(m);
+    if (limits) {
+      for (int round = 0; round < 2; ++round) {
+        mine = 0;
+        if (binned) {
+          clear_bins<THREADS>(sh, 0);
+          each(heavy{}, [&](float z, int e) {
+            if (real(z)) {
+              const int q = bin0(z);
+              if (by_k) atomicAdd(&sh.cnt[0][q], 1u);
+              atomicAdd(&sh.mass[0][q], wt.units(z));
+            }
+            set_aside(z, e, real(z) && z >= line);
+          });
+        } else {
+          each(light{}, [&](float z, int e) { set_aside(z, e, real(z) && z >= line); });
+        }
+        const bool fits = list_closed();
+        if (round == 0) listed = fits && (by_k ? n_list >= k || all : by_p || all);
+        if (listed || binned || !below_counts) break;
+        binned = true;  // a share of a k that the list does not reach
+      }
+      if (!listed && by_k && !by_p) {
+        clear_bins<THREADS>(sh, 0);
+        each(light{}, [&](float z, int) {
+          if (real(z)) atomicAdd(&sh.cnt[0][bin0(z)], 1u);
+        });
+        __syncthreads();
+        binned = true;
+      }
+    }
+
+    // The limits, ties and the draw, one after the other, each the pick of a value among ranked ones: of a
+    // logit by count (k) or by weight (p), of an id by count (ties at the cut) or by weight (the draw).
+    bool from_list = listed;  // else: from the list of a bin, or from the row itself
+    int bin_listed = -1;
+    uint32_t id_lim = 0xFFFFFFFFu;  // ids up to it are kept at the cut itself
+    u64 w_k = 0, total = 0;         // weight of the first k, or of all; of the kept
+    auto kept = [&](float z, int e) { return z > cut.z || (z == cut.z && (uint32_t)e <= id_lim); };
+#pragma unroll 1
+    for (int stage = 0; stage < 4; ++stage) {  // k, p, ties, draw
+      const bool up = stage >= 2;
+      // values of interest: above `from`, or at it with ids up to `to_id`; none above `upto`
+      float from = -INFINITY, upto = INFINITY;
+      uint32_t to_id = 0xFFFFFFFFu, lo = key_lo, hi = key_hi, c = 0, found = 0;
+      u64 w = 0;
+      Aim aim{stage == 1 || stage == 3, k};
+      if (stage == 0 && !by_k) continue;
+      if (stage == 1 && !by_p) continue;
+      if (stage == 2) {
+        if (cut.ties == ALL_TIES) continue;
+        if (!listed) from_list = bin_listed >= 0 && bin_listed == bin0(cut.z);
+        from = upto = cut.z;
+        aim.want = cut.ties;
+      }
+      if (stage == 3) {
+        if (!listed) break;
+        from = cut.z;
+        to_id = id_lim;
+      }
+      if (up) {
+        lo = 0;
+        hi = (uint32_t)a.V - 1;
+      }
+      auto visit = [&](auto f) {
+        each_listed([&](float z, int e) {
+          if ((z > from || (z == from && (uint32_t)e <= to_id)) && z <= upto) f(up ? (uint32_t)e : order_key(z), z);
+        });
+      };
+      auto visit_row = [&](auto f) {
+        each(single{}, [&](float z, int e) {
+          if (real(z) && z >= from && z <= upto) f(up ? (uint32_t)e : order_key(z), z);
+        });
+      };
+      if (!up && !listed) {
+        // narrowed to a bin of the row, whose logits become the list
+        if (stage == 1 && by_k) aim.want = share_of(w_k);
+        const int bin = find_bin<THREADS>(sh, 0, aim, c, w, [&](u64 sum) {
+          if (stage == 0 || !by_k) w_k = sum;
+          if (stage == 1 && !by_k) aim.want = share_of(sum);
+        });
+        if (bin < 0) continue;  // fewer than k can be drawn
+        mine = 0;
+        lo = 0xFFFFFFFFu;
+        hi = 0;
+        each(light{}, [&](float z, int e) {
+          const bool in = real(z) && bin0(z) == bin;
+          lo = min(lo, in ? order_key(z) : 0xFFFFFFFFu);
+          hi = max(hi, in ? order_key(z) : 0u);
+          set_aside(z, e, in);
+        });
+        block_range<NW>(lo, hi, sh);
+        from_list = list_closed();  // too long where many logits are equal: then from the row
+        bin_listed = from_list ? bin : -1;
+      } else {
+        uint32_t here = 0;
+        if (stage == 1 && by_k) {
+          if (n_list < k) {  // fewer than k: the share is of them all
+            visit([&](uint32_t, float z) { w_k += wt.units(z); });
+            block_sums<NW>(here, w_k, sh);
           }
-          before += sum;
+          aim.want = share_of(w_k);
+        } else if (stage == 1) {
+          // the bins of the row know the whole, and whether the list holds the cut (the line's own
+          // bin may lie on both of its sides)
+          const int bin = find_bin<THREADS>(sh, 0, aim = Aim{true, 0}, c, w,
+                                            [&](u64 sum) { aim.want = share_of(sum); });
+          const int line_bin = line == -INFINITY ? SAMPLE_BINS : bin0(line);
+          if (bin > line_bin && at_min_p) continue;  // min_p ends before top_p
+          if (bin >= line_bin) {
+            listed = false;
+            --stage;  // again, from the row's bins
+            continue;
+          }
+          c = 0;
+          w = 0;
+        } else if (stage == 2) {
+          if (from_list)
+            visit([&](uint32_t, float) { ++here; });
+          else
+            visit_row([&](uint32_t, float) { ++here; });
+          block_sums<NW>(here, total, sh);
+          total = 0;
+          if (cut.ties >= here) continue;
+        } else if (stage == 3) {
+          visit([&](uint32_t, float z) { total += wt.units(z); });
+          block_sums<NW>(here, total, sh);
+          aim.want = (u64)(u * (double)total) + 1;
+        }
+        if (!up && line == -INFINITY) {  // a short row: its range
+          lo = 0xFFFFFFFFu;
+          hi = 0;
+          visit([&](uint32_t q, float) {
+            lo = min(lo, q);
+            hi = max(hi, q);
+          });
+          block_range<NW>(lo, hi, sh);
         }
       }
-      __syncthreads();
-      if (sh.bin >= 0) id_lim = (uint32_t)sh.bin;
-      __syncthreads();
+      const bool reached = from_list ? pick<THREADS>(sh, wt, up, aim, lo, hi, c, w, found, visit)
+                                     : pick<THREADS>(sh, wt, up, aim, lo, hi, c, w, found, visit_row);
+      if (stage == 2) {
+        id_lim = found;
+      } else if (stage == 3) {
+        each_listed([&](float z, int e) {
+          if ((uint32_t)e == found) emit_drawn(z, e, total);
+        });
+      } else if (reached) {
+        const float z = key_value(found);
+        const u64 one = max(wt.units(z), 1ull);
+        const u64 ties = stage == 0 ? k - c : (aim.want - w + one - 1) / one;
+        if (stage == 0) w_k = w + ties * wt.units(z);
+        if (z > cut.z)
+          cut = {z, ties};
+        else if (z == cut.z)  // the shorter of two prefixes
+          cut.ties = min(cut.ties, ties);
+      }
     }
-    auto kept = [&](float z, int e) { return z > cut.z || (z == cut.z && (uint32_t)e <= id_lim); };
+    if (listed) continue;
 
-    // the draw: weights of each wave's run, in parts, then the part, the chunk and the token
-    const int per = (cpw + SAMPLE_GROUPS - 1) / SAMPLE_GROUPS;
-    u64 run = 0;
+    // the draw from the row: the weights of its parts, then of the chunks of the part that the number falls
+    // into, then the thread and the token
+    const int per = (cpt + SAMPLE_GROUPS - 1) / SAMPLE_GROUPS;
+    auto weight_of = [&](const float(&v)[EPC], int e0) {
+      u64 x = 0;
 #pragma unroll
+      for (int q = 0; q < EPC; ++q) {
+        const u64 w = wt.units(v[q]);
+        x += kept(v[q], e0 + q) ? w : 0;
+        if (q & 1) __builtin_amdgcn_sched_barrier(0);
+      }
+      return x;
+    };
+#pragma unroll 1
     for (int g = 0; g < SAMPLE_GROUPS; ++g) {
       u64 x = 0;
-      each(g * per, min(cpw, (g + 1) * per), [&](float z, int e) {
-        if (kept(z, e)) x += wt.units(z);
-      });
-      x = wave_sum_u64(x);
-      if (lane == 0) sh.group[wave][g] = x;
-      run += x;
+      chunks(heavy{}, g * per, min(cpt, (g + 1) * per),
+             [&](int, const float(&v)[EPC], int e0) { x += weight_of(v, e0); });
+      x = wave_total(x);
+      if (lane == 0) sh.part[g][wave] = x;
     }
-    if (lane == 0) sh.scan_m[wave] = run;
     __syncthreads();
-    u64 before = 0, total = 0;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) {
-      if (i < wave) before += sh.scan_m[i];
-      total += sh.scan_m[i];
-    }
-    const double u = fmin(fmax((double)a.uniform[o], 0.0), 1.0 - 0x1p-24);
+    total = 0;
+    for (int g = 0; g < SAMPLE_GROUPS; ++g)
+      for (int i = 0; i < NW; ++i) total += sh.part[g][i];
     const u64 want = (u64)(u * (double)total);  // the first cumulative weight above it
-    if (before <= want && before + run > want) {
-      int g = 0;
-      while (g + 1 < SAMPLE_GROUPS && before + sh.group[wave][g] <= want) before += sh.group[wave][g++];
-      for (int i = g * per; i < min(cpw, (g + 1) * per); ++i) {
-        u64 x = 0;
-        each(i, i + 1, [&](float z, int e) {
-          if (kept(z, e)) x += wt.units(z);
-        });
-        const u64 sum = wave_sum_u64(x);
-        if (before + sum > want) {
-          u64 at = before + wave_before_u64(x);
-          each(i, i + 1, [&](float z, int e) {
-            if (!kept(z, e)) return;
-            const u64 w = wt.units(z);
-            if (at <= want && at + w > want) {
-              const double lw = ((double)z - wt.m) * wt.c - log2((double)total) + wt.shift;
-              emit(e, (float)(lw * 0.69314718055994530942));
-            }
-            at += w;
-          });
-          break;
-        }
-        before += sum;
+    u64 before = 0;
+    int i0 = 0, i1 = cpt;
+    for (int g = 0; g < SAMPLE_GROUPS; ++g) {
+      u64 x = 0;
+      for (int i = 0; i < NW; ++i) x += sh.part[g][i];
+      if (before + x > want) {
+        i0 = g * per;
+        i1 = min(cpt, i0 + per);
+        break;
       }
+      before += x;
     }
-    __syncthreads();  // the shared arrays are written again for the next row
+    __syncthreads();
+    bool done = false;
+    for (int j0 = i0; j0 < i1 && !done; j0 += SAMPLE_STEPS) {
+      const int j1 = min(i1, j0 + SAMPLE_STEPS);
+      chunks(single{}, j0, j1, [&](int i, const float(&v)[EPC], int e0) {
+        const u64 x = wave_total(weight_of(v, e0));
+        if (lane == 0) sh.part[i - j0][wave] = x;
+      });
+      __syncthreads();
+      for (int i = j0; i < j1 && !done; ++i)
+        for (int h = 0; h < NW && !done; ++h) {
+          const u64 x = sh.part[i - j0][h];
+          if (before + x <= want) {
+            before += x;
+            continue;
+          }
+          done = true;
+          if (h != wave) break;
+          chunks(single{}, i, i + 1, [&](int, const float(&v)[EPC], int e0) {
+            const u64 own = weight_of(v, e0);
+            u64 at = before + wave_upto(own) - own;
+#pragma unroll
+            for (int q = 0; q < EPC; ++q)
+              if (kept(v[q], e0 + q)) {
+                const u64 w = wt.units(v[q]);
+                if (at <= want && at + w > want) emit_drawn(v[q], e0 + q, total);
+                at += w;
+              }
+          });
+        }
+      __syncthreads();
+    }
   }
 }
 
