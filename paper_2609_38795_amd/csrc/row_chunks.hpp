@@ -79,6 +79,32 @@ __device__ __forceinline__ void unpack(u32x4 w, float (&v)[RowChunks<T>::EPC]) {
   }
 }
 
+// f(i, c, chunk c) for the chunks c = c0 + i * STRIDE, i0 <= i < i1.  U loads go out ahead of the U chunks in
+// hand, so that a wave always has some under way.
+template <int U, int STRIDE, typename T, typename F>
+__device__ __forceinline__ void walk(const RowChunks<T>& row, int c0, int i0, int i1, F f) {
+  u32x4 w[U], next[U];
+  if (i0 >= i1) return;
+#pragma unroll
+  for (int u = 0; u < U; ++u) w[u] = row.load(c0 + (i0 + u) * STRIDE);
+#pragma unroll 1
+  for (int i = i0; i < i1; i += U) {
+    if (i + U < i1) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) next[u] = row.load(c0 + (i + U + u) * STRIDE);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i + u >= i1) break;
+      const int c = c0 + (i + u) * STRIDE;
+      f(i + u, c, row.whole(c, w[u]));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = next[u];
+  }
+}
+
 // Writes chunk c of a row that `g` describes to the row `out`, rounded once to T; vec: out's chunks
 // are 16-byte aligned where g's are.
 template <typename T>

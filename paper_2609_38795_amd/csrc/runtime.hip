@@ -65,6 +65,7 @@ struct Layout {
   size_t part_o, part_ml;
   size_t splitk, splitk_bytes;
   size_t qk_part;
+  size_t sample_rows, sample_hdr, sample_list, sample_seg, sample_part;
   size_t max_pwork, max_dwork, max_groups;
   size_t total;
 };
@@ -273,6 +274,12 @@ size_t compute_layout(const alr_config& c, const alr_limits& lim, Layout& L) {
   L.splitk_bytes = std::max(4 * NA, 8 * std::min<size_t>(NA, FEW_ROWS)) *
                    std::max(qd + 2 * kvd, d) * 4;
   L.splitk = take(L.splitk_bytes);
+  // what the scans of sampled rows leave, for a rollout's anchors at once
+  L.sample_rows = std::max<size_t>(1024, std::min<size_t>(NA, 2048));
+  L.sample_hdr = take(L.sample_rows * sizeof(SampleRow));
+  L.sample_list = take(L.sample_rows * SAMPLE_LIST * sizeof(f32x2));
+  L.sample_seg = take(L.sample_rows * SAMPLE_SEGS * sizeof(SampleSeg));
+  L.sample_part = take(L.sample_rows * SAMPLE_GROUPS * 8);
   // gain gradients of the q/k norms, one partial sum a workgroup
   L.qk_part = take((size_t)QK_BACK_WGS * 2 * hd * 4);
   L.total = off;
@@ -1237,13 +1244,31 @@ SampleArgs sample_args(const alr_sampling* sp, const float* uniform, int V) {
   return a;
 }
 
+// The scans of the rows, then the kernel that settles them, for as many rows at a time as the
+// scratch holds.
 template <typename T>
-void launch_sample(const SampleArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)std::min<long>(a.n, 1 << 20);
-  if (a.V > 8192)
-    sample_kernel<T, 512><<<grid, 512, 0, st>>>(a);
-  else
-    sample_kernel<T, 256><<<grid, 256, 0, st>>>(a);
+void launch_sample(const alr_ctx* ctx, SampleArgs a, hipStream_t st) {
+  const Layout& L = ctx->L;
+  const long n = a.n, cap = (long)L.sample_rows;
+  a.rows = ctx->at<SampleRow>(L.sample_hdr);
+  a.lists = ctx->at<f32x2>(L.sample_list);
+  a.segs = ctx->at<SampleSeg>(L.sample_seg);
+  a.parts = ctx->at<unsigned long long>(L.sample_part);
+  for (a.row0 = 0; a.row0 < n; a.row0 += cap) {
+    a.n = std::min(cap, n - a.row0);
+    // segments of at least two chunks a thread, 16 workgroups per CU where there are that many
+    a.n_seg = 1;
+    while (a.n_seg < SAMPLE_SEGS && a.n_seg * a.n < 16 * ctx->n_cu &&
+           (long)a.V * (long)sizeof(T) >= 2L * a.n_seg * 2 * 256 * 16)
+      a.n_seg *= 2;
+    const unsigned grid = (unsigned)(a.n * a.n_seg);
+    sample_scan_kernel<T, true><<<grid, 256, 0, st>>>(a);
+    sample_scan_kernel<T, false><<<grid, 256, 0, st>>>(a);
+    if (a.n <= ctx->n_cu)
+      sample_settle_kernel<T, 1024><<<(unsigned)a.n, 1024, 0, st>>>(a);
+    else
+      sample_settle_kernel<T, 512><<<(unsigned)a.n, 512, 0, st>>>(a);
+  }
 }
 
 // Output destinations of the labels of one rollout or corpus-label call.
@@ -1312,7 +1337,7 @@ alr_status lm_head(alr_ctx* ctx, int n, int s, int block, const int* forced, con
     sa.next_tok = ctx->at<int>(L.i_cur);
     sa.tokens = out.tokens;
     sa.logp = out.token_logp;
-    launch_sample<float>(sa, st);
+    launch_sample<float>(ctx, sa, st);
     ALR_LAUNCHED(ctx, "sampling");
     if (!out.top_ids && !out.logprobs) return ALR_OK;
   }
@@ -2259,9 +2284,9 @@ alr_status alr_sample(alr_ctx* ctx, int32_t n, int32_t vocab, const void* logits
   a.logp = logp_out;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (dtype == ALR_BF16)
-    launch_sample<bf16>(a, s);
+    launch_sample<bf16>(ctx, a, s);
   else
-    launch_sample<float>(a, s);
+    launch_sample<float>(ctx, a, s);
   ALR_LAUNCHED(ctx, "sampling");
   return ALR_OK;
 }

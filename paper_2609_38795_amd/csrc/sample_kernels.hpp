@@ -19,6 +19,8 @@
 
 namespace alr {
 
+typedef unsigned long long u64;
+
 struct SampleArgs {
   const void* z;
   long z_rs;
@@ -36,14 +38,50 @@ struct SampleArgs {
   int* next_tok;          // [r] or null: the token to feed
   int* tokens;
   float* logp;            // or null
+  // scratch of `cap` rows; a call of more rows comes in several, `row0` being the first of each
+  struct SampleRow* rows;
+  f32x2* lists;           // [cap, SAMPLE_LIST]
+  struct SampleSeg* segs; // [cap, SAMPLE_SEGS]
+  unsigned long long* parts;  // [cap, SAMPLE_GROUPS]
+  long row0;
+  int n_seg;              // segments of a row, each a workgroup's, in the scans
 };
 
-typedef unsigned long long u64;
-
 constexpr int SAMPLE_BINS = 1024, SAMPLE_BITS = 10;
-constexpr int SAMPLE_GROUPS = 8;    // parts of a row whose weights are summed apart for the draw
-constexpr int SAMPLE_STEPS = 16;    // chunks of a thread within one such part, at most
-constexpr int SAMPLE_LIST = 4096;   // logits that may be set aside
+constexpr int SAMPLE_GROUPS = 64;   // parts of a row whose weights are summed apart for the draw
+constexpr int SAMPLE_LIST = 4096;   // logits of a row that may be set aside
+constexpr int SAMPLE_SEGS = 16;     // segments of a row at most
+
+// What the scans of a row leave for the kernel that settles it.
+struct SampleRow {
+  u64 whole;        // weight of the row (a top_p of the whole row)
+  uint32_t n_list;  // logits set aside; more than SAMPLE_LIST: they did not fit
+  uint32_t greedy;  // lowest id at the maximum (greedy rows)
+  float m, line;
+};
+// Of a segment of a row: its maximum, and number, sum and sum of squares of the maxima of its parts.
+struct SampleSeg {
+  float m, c, s1, s2;
+};
+
+// A row's limits.
+struct Limits {
+  uint32_t k;
+  float temp, p, mp;
+  bool by_k, by_p, greedy, any;
+  __device__ __forceinline__ Limits(const SampleArgs& a, long idx, float m) {
+    temp = a.temperature ? a.temperature[idx] : 1.f;
+    k = a.top_k ? (uint32_t)max(a.top_k[idx], 0) : 0;
+    p = a.top_p ? a.top_p[idx] : 1.f;
+    mp = a.min_p ? a.min_p[idx] : 0.f;
+    by_k = k > 0 && k < (uint32_t)a.V;
+    by_p = p < 1.f;
+    greedy = !(temp > 0.f) || m == INFINITY;
+    any = by_k || by_p || mp > 0.f;
+  }
+  // top_p's share is of the first k, whether or not min_p ends before it
+  __device__ __forceinline__ bool below_counts() const { return by_k && by_p; }
+};
 
 // v of the lane that a DPP control names, 0 where there is none or the row is masked off
 template <int CTRL, int ROWS>
@@ -128,7 +166,10 @@ struct Weigher {
     shift = shift_;
     tab = tab_;
   }
-  __device__ __forceinline__ u64 units(float z) const {
+  static constexpr u64 BIAS = 0x4330000000000000ull;  // the bits of 2^52
+  __device__ __forceinline__ u64 units(float z) const { return biased(z) - BIAS; }
+  // units() + BIAS: what a long sum adds up, to take the biases off once at its end
+  __device__ __forceinline__ u64 biased(float z) const {
     constexpr double MAGIC = 6755399441055744.0, ONE52 = 4503599627370496.0;
     constexpr double L = 0.693147180559945309417232 / 32, A2 = 0.25;  // A2: (half width)^2
     constexpr double c5 = L * L * L * L * L / 120;
@@ -143,7 +184,7 @@ struct Weigher {
     p = fma(f, p, c2);
     p = fma(f, p, c1);
     p = fma(f, p, 1.0);
-    return (u64)__double_as_longlong(fma(p, __longlong_as_double((long long)w), ONE52)) & ((1ull << 52) - 1);
+    return (u64)__double_as_longlong(fma(p, __longlong_as_double((long long)w), ONE52));
   }
   __device__ __forceinline__ double log2_of(float z) const { return ((double)z - m) * c * (1.0 / 32); }
 };
@@ -155,27 +196,14 @@ struct SampleShared {
   f32x2 list[SAMPLE_LIST];       // (logit, id) of the logits set aside, a run of it per wave
   uint32_t scan_c[16], few_n;
   u64 scan_m[16];
-  u64 part[SAMPLE_STEPS][16];
+  u64 part[SAMPLE_GROUPS];
   uint32_t few_key[64];
   u64 few_w[64];
-  float fred[4][16];
   uint32_t ured[2][16];
   int bin;
   uint32_t above_c;
   u64 above_m;
 };
-
-template <int NW>
-__device__ __forceinline__ float block_max_f(float v, SampleShared& sh) {
-  v = wave_max(v);
-  if ((threadIdx.x & 63) == 0) sh.fred[0][threadIdx.x >> 6] = v;
-  __syncthreads();
-  float t = sh.fred[0][0];
-#pragma unroll
-  for (int i = 1; i < NW; ++i) t = fmaxf(t, sh.fred[0][i]);
-  __syncthreads();
-  return t;
-}
 
 // min and max of unsigned values over the workgroup
 template <int NW>
@@ -376,424 +404,563 @@ struct Cut {
 };
 constexpr u64 ALL_TIES = ~0ull;
 
-// One workgroup per row.  What bounds a row is its reads (the first from HBM, a second, where there is one,
-// mostly from the last-level cache) and, where every weight is needed, the 64-bit exponentials, about 15
-// operations each.
-//
-// Pass 1 takes the maximum, and the maxima of a thousand parts of the row: most of their spread lies
-// above the few thousandths of the row that limits usually keep.  Pass 2 sets the logits above a line drawn from
-// them aside (in LDS) and, for a top_p of the whole row, forms the histogram of the weights over (max - z) / T.
-// Limits that fall within the list are settled there, and so is the draw.  Others (a nucleus of a flat
-// distribution, a k of thousands) are narrowed to a bin of the histogram, the bin's logits are set aside
-// instead, and the draw reads the row again.
-//
+// The lowest float whose weight is at least min_p: near m + T ln p, then step by step.
+__device__ __forceinline__ float min_p_cut(const Weigher& wt, float m, float mp) {
+  const double want = fmin((double)mp, 1.0);
+  auto keeps = [&](float z) { return exp2(wt.log2_of(z)) >= want; };
+  const uint32_t top = order_key(m);
+  uint32_t key = min(order_key((float)fmax(wt.m + 32 * log2(want) / wt.c, -3.4e38)), top);
+  for (int i = 0; i < 64 && key < top && !keeps(key_value(key)); ++i) ++key;
+  for (int i = 0; i < 64 && key > 0x00800000u && keeps(key_value(key - 1)); ++i) --key;
+  return key_value(key);
+}
+
+__device__ __forceinline__ bool real(float z) { return z > -INFINITY; }  // neither nan nor -inf
+
 // Rows of different limits cost differently and limits tend to repeat, so a group of eight rows is dealt
 // to the eight XCDs in a rotating order.
+__device__ __forceinline__ long dealt_row(long b, long n) {
+  return (b | 7) < n ? (b & ~7L) | ((b + (b >> 3)) & 7) : b;
+}
+
+// A wave's run of logits set aside, in LDS.
+template <int RUN>
+struct Aside {
+  f32x2* run;
+  uint32_t mine = 0;
+  __device__ __forceinline__ explicit Aside(f32x2* r) : run(r) {}
+  // The logits of a chunk whose bit is set in `in`, one of every lane that has any left at a time: they
+  // are few, so one or two rounds do.
+  template <int EPC>
+  __device__ __forceinline__ void add(const float (&v)[EPC], int e0, uint32_t in) {
+    while (true) {
+      const u64 bits = __ballot(in != 0);
+      if (bits == 0) return;
+      const int q = __ffs((int)in) - 1;
+      float z = v[0];
+#pragma unroll
+      for (int i = 1; i < EPC; ++i) z = q == i ? v[i] : z;
+      const uint32_t at = mine + __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32),
+                                                          __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
+      if (in != 0 && at < RUN) run[at] = f32x2{z, __int_as_float(e0 + q)};
+      mine += (uint32_t)__popcll(bits);
+      in &= in - 1;
+    }
+  }
+};
+
+// First scan: every segment's maximum, and the statistics of the maxima of its parts, of which a row has
+// about a thousand (a segment of few chunks merges lanes).
+template <typename T>
+__device__ __forceinline__ SampleSeg scan_max(const RowChunks<T>& row, int n_seg, int seg, float (*red)[4]) {
+  constexpr int EPC = RowChunks<T>::EPC;
+  const int per = (row.nch + n_seg * 256 - 1) / (n_seg * 256);  // chunks of a thread
+  float part[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  walk<4, 256>(row, seg * per * 256 + (int)threadIdx.x, 0, per, [&](int i, int, u32x4 w) {
+    float v[EPC];
+    unpack<T>(w, v);
+    float x = v[0];
+#pragma unroll
+    for (int k = 1; k < EPC; ++k) x = fmaxf(x, v[k]);
+    const int h = i & 3;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) part[k] = fmaxf(part[k], h == k ? x : -INFINITY);
+  });
+  if (n_seg >= 2) {
+    part[0] = fmaxf(part[0], part[1]);
+    part[2] = fmaxf(part[2], part[3]);
+  }
+  if (n_seg >= 4) part[0] = fmaxf(part[0], part[2]);
+  if (n_seg >= 8) part[0] = fmaxf(part[0], dpp_perm<0xB1>(part[0]));
+  if (n_seg >= 16) part[0] = fmaxf(part[0], dpp_perm<0x4E>(part[0]));
+  SampleSeg s = {-INFINITY, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (k == 0 || (k == 2 && n_seg == 2) || n_seg == 1) {
+      s.m = fmaxf(s.m, part[k]);
+      if (part[k] != -INFINITY) {
+        s.c += 1.f;
+        s.s1 += part[k];
+        s.s2 += part[k] * part[k];
+      }
+    }
+  s.m = wave_max(s.m);
+  s.c = wave_sum(s.c);
+  s.s1 = wave_sum(s.s1);
+  s.s2 = wave_sum(s.s2);
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    red[wave][0] = s.m;
+    red[wave][1] = s.c;
+    red[wave][2] = s.s1;
+    red[wave][3] = s.s2;
+  }
+  __syncthreads();
+  s = {-INFINITY, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    s.m = fmaxf(s.m, red[i][0]);
+    s.c += red[i][1];
+    s.s1 += red[i][2];
+    s.s2 += red[i][3];
+  }
+  __syncthreads();
+  return s;
+}
+
+// The line: 1.5 standard deviations below the mean of the parts' maxima (an estimate: any line is right).
+__device__ __forceinline__ float line_of(const SampleSeg& s, int V) {
+  if (V <= SAMPLE_LIST / 2) return -INFINITY;
+  const float mean = s.s1 / s.c;
+  const float line = mean - 1.5f * sqrtf(fmaxf(s.s2 / s.c - mean * mean, 0.f));
+  return line == line ? line : -INFINITY;
+}
+
+struct ScanShared {
+  double tab[32];
+  f32x2 list[SAMPLE_LIST];
+  float red[4][4];
+  uint32_t n[4], base;
+};
+
+// Second scan: the logits above the line set aside; for a top_p of the whole row its weight; without limits,
+// the weights of the row's parts; for a greedy row the lowest id at the maximum.
+template <typename T>
+__device__ __forceinline__ void scan_list(const SampleArgs& a, const RowChunks<T>& row, int seg, long idx,
+                                          long slot, const SampleSeg& st, ScanShared& sh) {
+  constexpr int EPC = RowChunks<T>::EPC, RUN = SAMPLE_LIST / 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_seg = a.n_seg;
+  const float m = st.m;
+  SampleRow& hdr = a.rows[slot];
+  float line = line_of(st, a.V);
+  const Limits lim(a, idx, m);
+  Weigher wt;
+  wt.set(m, lim.temp, a.shift, sh.tab);
+  if (m != -INFINITY && !lim.greedy && lim.mp > 0.f && !lim.below_counts())
+    line = fmaxf(line, min_p_cut(wt, m, lim.mp));  // nothing below min_p counts
+  if (seg == 0 && threadIdx.x == 0) {
+    hdr.m = m;
+    hdr.line = line;
+  }
+  if (m == -INFINITY) return;
+  const int per = (row.nch + n_seg * 256 - 1) / (n_seg * 256), c0 = seg * per * 256 + (int)threadIdx.x;
+  if (lim.greedy) {
+    uint32_t lo = 0xFFFFFFFFu;
+    walk<4, 256>(row, c0, 0, per, [&](int, int c, u32x4 w) {
+      float v[EPC];
+      unpack<T>(w, v);
+#pragma unroll
+      for (int q = 0; q < EPC; ++q)
+        if (v[q] == m) lo = min(lo, (uint32_t)(row.first(c) + q));
+    });
+    if (lo != 0xFFFFFFFFu) atomicMin(&hdr.greedy, lo);
+    return;
+  }
+  if (!lim.any) {
+    const int gc = (row.nch + SAMPLE_GROUPS - 1) / SAMPLE_GROUPS, steps = (gc + 63) / 64;
+    for (int g = seg * (SAMPLE_GROUPS / n_seg) + wave; g < (seg + 1) * (SAMPLE_GROUPS / n_seg); g += 4) {
+      u64 x = 0;
+      walk<4, 64>(row, g * gc + lane, 0, steps, [&](int, int c, u32x4 w) {
+        float v[EPC];
+        unpack<T>(w, v);
+        u64 y = 0;
+#pragma unroll
+        for (int q = 0; q < EPC; ++q) y += wt.biased(v[q]);
+        x += c < (g + 1) * gc ? y - EPC * Weigher::BIAS : 0;
+      });
+      x = wave_total(x);
+      if (lane == 0) a.parts[slot * SAMPLE_GROUPS + g] = x;
+    }
+    return;
+  }
+  Aside<RUN> aside(sh.list + wave * RUN);
+  const float bound = fmaxf(line, -3.402823466e38f);  // -inf is never kept
+  if (lim.by_p && !lim.by_k) {
+    u64 x = 0;
+    walk<4, 256>(row, c0, 0, per, [&](int, int c, u32x4 w) {
+      float v[EPC];
+      uint32_t in = 0;
+      unpack<T>(w, v);
+#pragma unroll
+      for (int q = 0; q < EPC; ++q) {
+        x += wt.biased(v[q]);
+        in |= v[q] >= bound ? 1u << q : 0;
+      }
+      aside.add(v, row.first(c), in);
+    });
+    x = wave_total(x - (u64)(per * EPC) * Weigher::BIAS);
+    if (lane == 0) atomicAdd(&hdr.whole, x);
+  } else {
+    walk<4, 256>(row, c0, 0, per, [&](int, int c, u32x4 w) {
+      float v[EPC];
+      uint32_t in = 0;
+      unpack<T>(w, v);
+#pragma unroll
+      for (int q = 0; q < EPC; ++q) in |= v[q] >= bound ? 1u << q : 0;
+      aside.add(v, row.first(c), in);
+    });
+  }
+  if (lane == 0) sh.n[wave] = aside.mine;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t n = 0;
+    bool fits = true;
+    for (int i = 0; i < 4; ++i) {
+      n += sh.n[i];
+      fits &= sh.n[i] <= RUN;
+    }
+    // what does not fit puts the count out of reach (it stays below 2^32: segments are few)
+    sh.base = n ? atomicAdd(&hdr.n_list, fits ? n : SAMPLE_LIST + 1u) : 0;
+  }
+  __syncthreads();
+  uint32_t at = sh.base;
+  for (int i = 0; i < wave; ++i) at += sh.n[i];
+  for (uint32_t i = lane; i < min(aside.mine, (uint32_t)RUN); i += 64)
+    if (at + i < SAMPLE_LIST) a.lists[slot * SAMPLE_LIST + at + i] = aside.run[i];
+  __syncthreads();
+}
+
+// The first (FIRST) and the second scan, a.n_seg workgroups a row.  Both walk the segments in opposite
+// orders: the second begins with what the last-level cache still holds of the first.
+template <typename T, bool FIRST>
+__global__ __launch_bounds__(256, 4) void sample_scan_kernel(SampleArgs a) {
+  __shared__ ScanShared sh;
+  if (!FIRST && threadIdx.x < 32) sh.tab[threadIdx.x] = exp2((double)threadIdx.x / 32 + a.shift);
+  const long wg = FIRST ? blockIdx.x : gridDim.x - 1 - blockIdx.x, b = wg / a.n_seg;
+  const int seg = (int)(wg - b * a.n_seg);
+  const long slot = dealt_row(b, a.n), r = a.row0 + slot, idx = a.perm ? (long)a.perm[r] : r;
+  RowChunks<T> row(static_cast<const T*>(a.z) + (a.z_perm ? idx : r) * a.z_rs, a.V);
+  row.edges();
+  SampleSeg s;
+  if constexpr (FIRST) {
+    s = scan_max(row, a.n_seg, seg, sh.red);
+    if (threadIdx.x != 0) return;
+    if (seg == 0) {
+      a.rows[slot].whole = 0;
+      a.rows[slot].n_list = 0;
+      a.rows[slot].greedy = 0xFFFFFFFFu;
+    }
+    a.segs[slot * SAMPLE_SEGS + seg] = s;
+  } else {
+    s = {-INFINITY, 0.f, 0.f, 0.f};
+    for (int i = 0; i < a.n_seg; ++i) {
+      const SampleSeg x = a.segs[slot * SAMPLE_SEGS + i];
+      s.m = fmaxf(s.m, x.m);
+      s.c += x.c;
+      s.s1 += x.s1;
+      s.s2 += x.s2;
+    }
+    __syncthreads();  // the table
+    scan_list(a, row, seg, idx, slot, s, sh);
+  }
+}
+
+// Settles a row from what the scans left.  Limits that fall within the list are settled there, and so is the
+// draw.  Others (a nucleus of a flat distribution, a k of thousands) take a histogram of the row, the list
+// becomes that of the bin they fall into, and the draw reads the row again.  Without limits only the part of
+// the row that the number falls into is read again.
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleArgs a) {
+__global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a) {
   constexpr int NW = THREADS / 64, EPC = RowChunks<T>::EPC, RUN = SAMPLE_LIST / NW;
   static_assert(SAMPLE_BINS % THREADS == 0 && NW <= 16, "bins per thread");
   __shared__ SampleShared sh;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long slot = dealt_row(blockIdx.x, a.n), r = a.row0 + slot;
+  const long idx = a.perm ? (long)a.perm[r] : r, o = idx * a.block + a.s;
+  auto emit = [&](int tok, float lp) {
+    a.tokens[o] = tok;
+    if (a.logp) a.logp[o] = lp;
+    if (a.next_tok) {
+      const int f = a.forced ? a.forced[o] : -1;
+      a.next_tok[r] = f >= 0 ? f : max(tok, 0);
+    }
+  };
+  const SampleRow hdr = a.rows[slot];
+  const float m = hdr.m, line = hdr.line;
+  if (m == -INFINITY) {  // nothing to draw
+    if (threadIdx.x == 0) emit(-1, -INFINITY);
+    return;
+  }
+  const Limits lim(a, idx, m);
+  if (lim.greedy) {
+    if (threadIdx.x == 0) emit((int)hdr.greedy, 0.f);
+    return;
+  }
   if (threadIdx.x < 32) sh.tab[threadIdx.x] = exp2((double)threadIdx.x / 32 + a.shift);
-  for (long b = blockIdx.x; b < a.n; b += gridDim.x) {
-    const long r = (b | 7) < a.n ? (b & ~7L) | ((b + (b >> 3)) & 7) : b;
-    const long idx = a.perm ? (long)a.perm[r] : r, o = idx * a.block + a.s;
-    RowChunks<T> row(static_cast<const T*>(a.z) + (a.z_perm ? idx : r) * a.z_rs, a.V);
-    row.edges();
-    // thread t's chunk i is i * THREADS + t: ids rise with i, then with the thread
-    const int cpt = (row.nch + THREADS - 1) / THREADS;
-    // f(i, logits, first id) for chunks [i0, i1) of the thread, U loads in flight
-    auto chunks = [&](auto u_, int i0, int i1, auto f) {
-      constexpr int U = decltype(u_)::value;
-#pragma unroll 1
-      for (int i = i0; i < i1; i += U) {
-        u32x4 w[U];
+  __syncthreads();
+  Weigher wt;
+  wt.set(m, lim.temp, a.shift, sh.tab);
+  RowChunks<T> row(static_cast<const T*>(a.z) + (a.z_perm ? idx : r) * a.z_rs, a.V);
+  const int cpt = (row.nch + THREADS - 1) / THREADS;
+  // f(logits, first id) for the thread's chunks
+  auto chunks = [&](auto u_, auto f) {
+    walk<decltype(u_)::value, THREADS>(row, (int)threadIdx.x, 0, cpt, [&](int, int c, u32x4 w) {
+      float v[EPC];
+      unpack<T>(w, v);
+      f(v, row.first(c));
+    });
+  };
+  using light = std::integral_constant<int, 4>;
+  using heavy = std::integral_constant<int, 4>;  // passes that weigh every logit
+  auto each = [&](auto u_, auto f) {
+    chunks(u_, [&](const float(&v)[EPC], int e0) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = row.load((i + u) * THREADS + (int)threadIdx.x);
+      for (int k = 0; k < EPC; ++k) f(v[k], e0 + k);
+    });
+  };
+  const uint32_t k = lim.k;
+  const bool by_k = lim.by_k, by_p = lim.by_p;
+  auto share_of = [&](u64 w) { return max((u64)ceil(fmax((double)lim.p, 0.0) * (double)w), 1ull); };
+  const double u = fmin(fmax((double)a.uniform[o], 0.0), 1.0 - 0x1p-24);
+  auto emit_drawn = [&](float z, int e, u64 total) {
+    emit(e, (float)((wt.log2_of(z) + wt.shift - log2((double)total)) * 0.69314718055994530942));
+  };
+
+  Cut cut = {-INFINITY, ALL_TIES};
+  if (lim.mp > 0.f) cut.z = min_p_cut(wt, m, lim.mp);
+  uint32_t id_lim = 0xFFFFFFFFu;  // ids up to it are kept at the cut itself
+  auto kept = [&](float z, int e) { return z > cut.z || (z == cut.z && (uint32_t)e <= id_lim); };
+
+  Aside<RUN> aside(sh.list + wave * RUN);
+  uint32_t n_list = 0;
+  auto each_listed = [&](auto f) {
+    for (uint32_t i = lane; i < aside.mine; i += 64) {
+      const f32x2 x = aside.run[i];
+      f(x[0], __float_as_int(x[1]));
+    }
+  };
+  auto list_closed = [&]() {  // whether every wave's share fitted its run
+    if (lane == 0) sh.scan_c[wave] = aside.mine;
+    __syncthreads();
+    bool fits = true;
+    n_list = 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (i + u >= i1) break;
-          const int c = (i + u) * THREADS + (int)threadIdx.x;
-          float v[EPC];
-          unpack<T>(row.whole(c, w[u]), v);
-          f(i + u, v, row.first(c));
-        }
-      }
-    };
-    using light = std::integral_constant<int, 8>;
-    using heavy = std::integral_constant<int, 2>;  // passes that weigh every logit
-    using single = std::integral_constant<int, 1>;
-    // f(logit, id) over the row.  Weights take many registers: two at a time are enough to fill the
-    // pipeline with four waves per SIMD.
-    auto each = [&](auto u_, auto f) {
-      chunks(u_, 0, cpt, [&](int, const float(&v)[EPC], int e0) {
-#pragma unroll
-        for (int k = 0; k < EPC; ++k) {
-          f(v[k], e0 + k);
-          if (decltype(u_)::value <= 2 && (k & 1)) __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < NW; ++i) {
+      fits &= sh.scan_c[i] <= RUN;
+      n_list += sh.scan_c[i];
+    }
+    __syncthreads();
+    return fits;
+  };
+  // bins of the whole row, of 1/32 in (max - z) / T, the last one for all that lies below
+  const float cs = fminf(32.f / lim.temp, 1e30f);
+  auto bin0 = [&](float z) { return (int)fminf((m - z) * cs, (float)(SAMPLE_BINS - 1)); };
+  bool binned = false;
+  auto bin_row = [&]() {
+    clear_bins<THREADS>(sh, 0);
+    if (by_p)
+      each(heavy{}, [&](float z, int) {
+        if (real(z)) {
+          const int q = bin0(z);
+          if (by_k) atomicAdd(&sh.cnt[0][q], 1u);
+          atomicAdd(&sh.mass[0][q], wt.units(z));
         }
       });
-    };
-    auto emit = [&](int tok, float lp) {
-      a.tokens[o] = tok;
-      if (a.logp) a.logp[o] = lp;
-      if (a.next_tok) {
-        const int f = a.forced ? a.forced[o] : -1;
-        a.next_tok[r] = f >= 0 ? f : max(tok, 0);
-      }
-    };
+    else
+      each(light{}, [&](float z, int) {
+        if (real(z)) atomicAdd(&sh.cnt[0][bin0(z)], 1u);
+      });
+    __syncthreads();
+    binned = true;
+  };
 
-    // pass 1
-    float part[2] = {-INFINITY, -INFINITY};
-    chunks(light{}, 0, cpt, [&](int i, const float(&v)[EPC], int) {
-#pragma unroll
-      for (int k = 0; k < EPC; ++k) part[i & 1] = fmaxf(part[i & 1], v[k]);
-    });
-    const float m = block_max_f<NW>(fmaxf(part[0], part[1]), sh);
-    if (m == -INFINITY) {  // nothing to draw
-      if (threadIdx.x == 0) emit(-1, -INFINITY);
-      continue;
+  const bool fits = hdr.n_list <= SAMPLE_LIST;
+  // what is not listed is not kept: the list is the row, or ends where min_p does
+  const bool all = line == -INFINITY || (!lim.below_counts() && cut.z >= line);
+  // listed: every logit that may be kept is in the list (and the limits are settled there)
+  bool listed = lim.any && fits && (by_k ? hdr.n_list >= k || all : by_p || all);
+  if (listed) {
+    n_list = hdr.n_list;
+    for (uint32_t i = threadIdx.x; i < n_list; i += THREADS)
+      aside.run[i / THREADS * 64 + lane] = a.lists[slot * SAMPLE_LIST + i];
+    const uint32_t rest = n_list % THREADS, skip = (uint32_t)wave * 64;
+    aside.mine = n_list / THREADS * 64 + (rest > skip ? min(rest - skip, 64u) : 0);
+  }
+  u64 w_k = hdr.whole, total = 0;  // weight of the first k, or of all; of the kept
+
+  // The limits, ties and the draw, one after the other, each the pick of a value among ranked ones: of a
+  // logit by count (k) or by weight (p), of an id by count (ties at the cut) or by weight (the draw).
+  bool from_list = listed;  // else: from the list of a bin, or from the row itself
+  int bin_listed = -1;
+#pragma unroll 1
+  for (int stage = lim.any ? 0 : 4; stage < 4; ++stage) {  // k, p, ties, draw
+    const bool up = stage >= 2;
+    // values of interest: above `from`, or at it with ids up to `to_id`; none above `upto`
+    float from = -INFINITY, upto = INFINITY;
+    uint32_t to_id = 0xFFFFFFFFu, lo = order_key(line), hi = order_key(m), c = 0, found = 0;
+    u64 w = 0;
+    Aim aim{stage == 1 || stage == 3, k};
+    if (stage == 0 && !by_k) continue;
+    if (stage == 1 && !by_p) continue;
+    if (stage == 2) {
+      if (cut.ties == ALL_TIES) continue;
+      if (!listed) from_list = bin_listed >= 0 && bin_listed == bin0(cut.z);
+      from = upto = cut.z;
+      aim.want = cut.ties;
     }
-    const float temp = a.temperature ? a.temperature[idx] : 1.f;
-    if (!(temp > 0.f) || m == INFINITY) {  // greedy: the lowest id at the maximum
-      uint32_t lo = 0xFFFFFFFFu, hi = 0;
-      each(light{}, [&](float z, int e) {
-        if (z == m) lo = min(lo, (uint32_t)e);
+    if (stage == 3) {
+      if (!listed) break;
+      from = cut.z;
+      to_id = id_lim;
+    }
+    if (up) {
+      lo = 0;
+      hi = (uint32_t)a.V - 1;
+    }
+    auto visit = [&](auto f) {
+      each_listed([&](float z, int e) {
+        if ((z > from || (z == from && (uint32_t)e <= to_id)) && z <= upto) f(up ? (uint32_t)e : order_key(z), z);
+      });
+    };
+    auto visit_row = [&](auto f) {
+      each(std::integral_constant<int, 1>{}, [&](float z, int e) {
+        if (real(z) && z >= from && z <= upto) f(up ? (uint32_t)e : order_key(z), z);
+      });
+    };
+    if (!listed) row.edges();
+    if (!up && !listed) {
+      // narrowed to a bin of the row, whose logits become the list
+      if (!binned) bin_row();
+      if (stage == 1) aim.want = share_of(w_k);
+      const int bin = find_bin<THREADS>(sh, 0, aim, c, w, [&](u64 sum) {
+        if (stage == 0) w_k = sum;
+      });
+      if (bin < 0) continue;  // fewer than k can be drawn
+      aside.mine = 0;
+      lo = 0xFFFFFFFFu;
+      hi = 0;
+      chunks(light{}, [&](const float(&v)[EPC], int e0) {
+        uint32_t in = 0;
+#pragma unroll
+        for (int q = 0; q < EPC; ++q) {
+          const bool is = real(v[q]) && bin0(v[q]) == bin;
+          lo = min(lo, is ? order_key(v[q]) : 0xFFFFFFFFu);
+          hi = max(hi, is ? order_key(v[q]) : 0u);
+          in |= is ? 1u << q : 0;
+        }
+        aside.add(v, e0, in);
       });
       block_range<NW>(lo, hi, sh);
-      if (threadIdx.x == 0) emit((int)lo, 0.f);
-      continue;
-    }
-    Weigher wt;
-    wt.set(m, temp, a.shift, sh.tab);
-    const uint32_t k = a.top_k ? (uint32_t)max(a.top_k[idx], 0) : 0;
-    const float p = a.top_p ? a.top_p[idx] : 1.f, mp = a.min_p ? a.min_p[idx] : 0.f;
-    const bool by_k = k > 0 && k < (uint32_t)a.V, by_p = p < 1.f;
-    const double share = fmax((double)p, 0.0);
-    const double u = fmin(fmax((double)a.uniform[o], 0.0), 1.0 - 0x1p-24);
-    auto share_of = [&](u64 w) { return max((u64)ceil(share * (double)w), 1ull); };
-    auto emit_drawn = [&](float z, int e, u64 total) {
-      emit(e, (float)((wt.log2_of(z) + wt.shift - log2((double)total)) * 0.69314718055994530942));
-    };
-
-    Cut cut = {-INFINITY, ALL_TIES};
-    if (mp > 0.f) {
-      // the lowest float whose weight is at least min_p: near m + T ln p, then step by step
-      const double want = fmin((double)mp, 1.0);
-      auto keeps = [&](float z) { return exp2(wt.log2_of(z)) >= want; };
-      const uint32_t top = order_key(m);
-      uint32_t key = min(order_key((float)fmax(wt.m + 32 * log2(want) / wt.c, -3.4e38)), top);
-      for (int i = 0; i < 64 && key < top && !keeps(key_value(key)); ++i) ++key;
-      for (int i = 0; i < 64 && key > 0x00800000u && keeps(key_value(key - 1)); ++i) --key;
-      cut.z = key_value(key);
-    }
-
-    // pass 2: the list of logits >= line, each wave's share in its own run
-    uint32_t mine = 0, n_list = 0;  // entries of this wave, of all
-    auto set_aside = [&](float z, int e, bool in) {
-      const u64 bits = __ballot(in);
-      if (bits == 0) return;
-      const uint32_t at = mine + __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32),
-                                                          __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
-      if (in && at < RUN) sh.list[wave * RUN + at] = f32x2{z, __int_as_float(e)};
-      mine += (uint32_t)__popcll(bits);
-    };
-    auto each_listed = [&](auto f) {
-      for (uint32_t i = lane; i < mine; i += 64) {
-        const f32x2 x = sh.list[wave * RUN + i];
-        f(x[0], __float_as_int(x[1]));
-      }
-    };
-    auto list_closed = [&]() {  // whether every wave's share fitted its run
-      if (lane == 0) sh.scan_c[wave] = mine;
-      __syncthreads();
-      bool fits = true;
-      n_list = 0;
-#pragma unroll
-      for (int i = 0; i < NW; ++i) {
-        fits &= sh.scan_c[i] <= RUN;
-        n_list += sh.scan_c[i];
-      }
-      __syncthreads();
-      return fits;
-    };
-    auto real = [](float z) { return z > -INFINITY; };  // neither nan nor -inf
-    // bins of 1/32 in (max - z) / T, the last one for all that lies below
-    const float cs = fminf(32.f / temp, 1e30f);
-    auto bin0 = [&](float z) { return (int)fminf((m - z) * cs, (float)(SAMPLE_BINS - 1)); };
-    const bool limits = by_k || by_p || mp > 0.f;
-    // the line: 1.5 standard deviations below the mean of the parts' maxima (an estimate, any line is
-    // right), or where min_p ends if nothing below counts
-    float line = -INFINITY;
-    if (limits && a.V > SAMPLE_LIST / 2) {
-      float c = 0.f, s1 = 0.f, s2 = 0.f;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (part[h] != -INFINITY) {
-          const float d = m - part[h];
-          c += 1.f;
-          s1 += d;
-          s2 += d * d;
+      from_list = list_closed();  // too long where many logits are equal: then from the row
+      bin_listed = from_list ? bin : -1;
+    } else {
+      uint32_t here = 0;
+      if (stage == 1) {
+        if (by_k && n_list < k) {  // fewer than k: the share is of them all
+          w_k = 0;
+          visit([&](uint32_t, float z) { w_k += wt.units(z); });
+          block_sums<NW>(here, w_k, sh);
         }
-      c = wave_sum(c);
-      s1 = wave_sum(s1);
-      s2 = wave_sum(s2);
-      if (lane == 0) {
-        sh.fred[1][wave] = c;
-        sh.fred[2][wave] = s1;
-        sh.fred[3][wave] = s2;
+        aim.want = share_of(w_k);
+      } else if (stage == 2) {
+        if (from_list)
+          visit([&](uint32_t, float) { ++here; });
+        else
+          visit_row([&](uint32_t, float) { ++here; });
+        block_sums<NW>(here, total, sh);
+        total = 0;
+        if (cut.ties >= here) continue;
+      } else if (stage == 3) {
+        visit([&](uint32_t, float z) { total += wt.units(z); });
+        block_sums<NW>(here, total, sh);
+        aim.want = (u64)(u * (double)total) + 1;
       }
-      __syncthreads();
-      c = s1 = s2 = 0.f;
-#pragma unroll
-      for (int i = 0; i < NW; ++i) {
-        c += sh.fred[1][i];
-        s1 += sh.fred[2][i];
-        s2 += sh.fred[3][i];
-      }
-      __syncthreads();
-      const float mean = s1 / c;
-      line = m - (mean + 1.5f * sqrtf(fmaxf(s2 / c - mean * mean, 0.f)));
-    }
-    const bool below_counts = by_k && by_p;  // top_p's share is of the first k, min_p or not
-    const bool at_min_p = limits && !below_counts && cut.z >= line;
-    if (at_min_p) line = cut.z;
-    const bool all = line == -INFINITY || at_min_p;  // what is not listed is not kept
-    // listed: every logit that may be kept is in the list (and the limits are settled there).  With a
-    // top_p of the whole row, or where the list turns out too short, the first level of bins over the row.
-    bool listed = false, binned = by_p && !by_k;
-    uint32_t key_lo = order_key(line), key_hi = order_key(m);
-    if (limits) {
-      for (int round = 0; round < 2; ++round) {
-        mine = 0;
-        if (binned) {
-          clear_bins<THREADS>(sh, 0);
-          each(heavy{}, [&](float z, int e) {
-            if (real(z)) {
-              const int q = bin0(z);
-              if (by_k) atomicAdd(&sh.cnt[0][q], 1u);
-              atomicAdd(&sh.mass[0][q], wt.units(z));
-            }
-            set_aside(z, e, real(z) && z >= line);
-          });
-        } else {
-          each(light{}, [&](float z, int e) { set_aside(z, e, real(z) && z >= line); });
-        }
-        const bool fits = list_closed();
-        if (round == 0) listed = fits && (by_k ? n_list >= k || all : by_p || all);
-        if (listed || binned || !below_counts) break;
-        binned = true;  // a share of a k that the list does not reach
-      }
-      if (!listed && by_k && !by_p) {
-        clear_bins<THREADS>(sh, 0);
-        each(light{}, [&](float z, int) {
-          if (real(z)) atomicAdd(&sh.cnt[0][bin0(z)], 1u);
-        });
-        __syncthreads();
-        binned = true;
-      }
-    }
-
-    // The limits, ties and the draw, one after the other, each the pick of a value among ranked ones: of a
-    // logit by count (k) or by weight (p), of an id by count (ties at the cut) or by weight (the draw).
-    bool from_list = listed;  // else: from the list of a bin, or from the row itself
-    int bin_listed = -1;
-    uint32_t id_lim = 0xFFFFFFFFu;  // ids up to it are kept at the cut itself
-    u64 w_k = 0, total = 0;         // weight of the first k, or of all; of the kept
-    auto kept = [&](float z, int e) { return z > cut.z || (z == cut.z && (uint32_t)e <= id_lim); };
-#pragma unroll 1
-    for (int stage = 0; stage < 4; ++stage) {  // k, p, ties, draw
-      const bool up = stage >= 2;
-      // values of interest: above `from`, or at it with ids up to `to_id`; none above `upto`
-      float from = -INFINITY, upto = INFINITY;
-      uint32_t to_id = 0xFFFFFFFFu, lo = key_lo, hi = key_hi, c = 0, found = 0;
-      u64 w = 0;
-      Aim aim{stage == 1 || stage == 3, k};
-      if (stage == 0 && !by_k) continue;
-      if (stage == 1 && !by_p) continue;
-      if (stage == 2) {
-        if (cut.ties == ALL_TIES) continue;
-        if (!listed) from_list = bin_listed >= 0 && bin_listed == bin0(cut.z);
-        from = upto = cut.z;
-        aim.want = cut.ties;
-      }
-      if (stage == 3) {
-        if (!listed) break;
-        from = cut.z;
-        to_id = id_lim;
-      }
-      if (up) {
-        lo = 0;
-        hi = (uint32_t)a.V - 1;
-      }
-      auto visit = [&](auto f) {
-        each_listed([&](float z, int e) {
-          if ((z > from || (z == from && (uint32_t)e <= to_id)) && z <= upto) f(up ? (uint32_t)e : order_key(z), z);
-        });
-      };
-      auto visit_row = [&](auto f) {
-        each(single{}, [&](float z, int e) {
-          if (real(z) && z >= from && z <= upto) f(up ? (uint32_t)e : order_key(z), z);
-        });
-      };
-      if (!up && !listed) {
-        // narrowed to a bin of the row, whose logits become the list
-        if (stage == 1 && by_k) aim.want = share_of(w_k);
-        const int bin = find_bin<THREADS>(sh, 0, aim, c, w, [&](u64 sum) {
-          if (stage == 0 || !by_k) w_k = sum;
-          if (stage == 1 && !by_k) aim.want = share_of(sum);
-        });
-        if (bin < 0) continue;  // fewer than k can be drawn
-        mine = 0;
+      if (!up && line == -INFINITY) {  // a short row: its range
         lo = 0xFFFFFFFFu;
         hi = 0;
-        each(light{}, [&](float z, int e) {
-          const bool in = real(z) && bin0(z) == bin;
-          lo = min(lo, in ? order_key(z) : 0xFFFFFFFFu);
-          hi = max(hi, in ? order_key(z) : 0u);
-          set_aside(z, e, in);
+        visit([&](uint32_t q, float) {
+          lo = min(lo, q);
+          hi = max(hi, q);
         });
         block_range<NW>(lo, hi, sh);
-        from_list = list_closed();  // too long where many logits are equal: then from the row
-        bin_listed = from_list ? bin : -1;
-      } else {
-        uint32_t here = 0;
-        if (stage == 1 && by_k) {
-          if (n_list < k) {  // fewer than k: the share is of them all
-            visit([&](uint32_t, float z) { w_k += wt.units(z); });
-            block_sums<NW>(here, w_k, sh);
-          }
-          aim.want = share_of(w_k);
-        } else if (stage == 1) {
-          // the bins of the row know the whole, and whether the list holds the cut (the line's own
-          // bin may lie on both of its sides)
-          const int bin = find_bin<THREADS>(sh, 0, aim = Aim{true, 0}, c, w,
-                                            [&](u64 sum) { aim.want = share_of(sum); });
-          const int line_bin = line == -INFINITY ? SAMPLE_BINS : bin0(line);
-          if (bin > line_bin && at_min_p) continue;  // min_p ends before top_p
-          if (bin >= line_bin) {
-            listed = false;
-            --stage;  // again, from the row's bins
-            continue;
-          }
-          c = 0;
-          w = 0;
-        } else if (stage == 2) {
-          if (from_list)
-            visit([&](uint32_t, float) { ++here; });
-          else
-            visit_row([&](uint32_t, float) { ++here; });
-          block_sums<NW>(here, total, sh);
-          total = 0;
-          if (cut.ties >= here) continue;
-        } else if (stage == 3) {
-          visit([&](uint32_t, float z) { total += wt.units(z); });
-          block_sums<NW>(here, total, sh);
-          aim.want = (u64)(u * (double)total) + 1;
-        }
-        if (!up && line == -INFINITY) {  // a short row: its range
-          lo = 0xFFFFFFFFu;
-          hi = 0;
-          visit([&](uint32_t q, float) {
-            lo = min(lo, q);
-            hi = max(hi, q);
-          });
-          block_range<NW>(lo, hi, sh);
-        }
-      }
-      const bool reached = from_list ? pick<THREADS>(sh, wt, up, aim, lo, hi, c, w, found, visit)
-                                     : pick<THREADS>(sh, wt, up, aim, lo, hi, c, w, found, visit_row);
-      if (stage == 2) {
-        id_lim = found;
-      } else if (stage == 3) {
-        each_listed([&](float z, int e) {
-          if ((uint32_t)e == found) emit_drawn(z, e, total);
-        });
-      } else if (reached) {
-        const float z = key_value(found);
-        const u64 one = max(wt.units(z), 1ull);
-        const u64 ties = stage == 0 ? k - c : (aim.want - w + one - 1) / one;
-        if (stage == 0) w_k = w + ties * wt.units(z);
-        if (z > cut.z)
-          cut = {z, ties};
-        else if (z == cut.z)  // the shorter of two prefixes
-          cut.ties = min(cut.ties, ties);
       }
     }
-    if (listed) continue;
-
-    // the draw from the row: the weights of its parts, then of the chunks of the part that the number falls
-    // into, then the thread and the token
-    const int per = (cpt + SAMPLE_GROUPS - 1) / SAMPLE_GROUPS;
-    auto weight_of = [&](const float(&v)[EPC], int e0) {
-      u64 x = 0;
-#pragma unroll
-      for (int q = 0; q < EPC; ++q) {
-        const u64 w = wt.units(v[q]);
-        x += kept(v[q], e0 + q) ? w : 0;
-        if (q & 1) __builtin_amdgcn_sched_barrier(0);
-      }
-      return x;
-    };
-#pragma unroll 1
-    for (int g = 0; g < SAMPLE_GROUPS; ++g) {
-      u64 x = 0;
-      chunks(heavy{}, g * per, min(cpt, (g + 1) * per),
-             [&](int, const float(&v)[EPC], int e0) { x += weight_of(v, e0); });
-      x = wave_total(x);
-      if (lane == 0) sh.part[g][wave] = x;
+    const bool reached = from_list ? pick<THREADS>(sh, wt, up, aim, lo, hi, c, w, found, visit)
+                                   : pick<THREADS>(sh, wt, up, aim, lo, hi, c, w, found, visit_row);
+    if (!reached && stage == 1 && !all) {  // the list ends before top_p does
+      listed = false;
+      --stage;
+      continue;
     }
-    __syncthreads();
-    total = 0;
-    for (int g = 0; g < SAMPLE_GROUPS; ++g)
-      for (int i = 0; i < NW; ++i) total += sh.part[g][i];
-    const u64 want = (u64)(u * (double)total);  // the first cumulative weight above it
-    u64 before = 0;
-    int i0 = 0, i1 = cpt;
-    for (int g = 0; g < SAMPLE_GROUPS; ++g) {
-      u64 x = 0;
-      for (int i = 0; i < NW; ++i) x += sh.part[g][i];
-      if (before + x > want) {
-        i0 = g * per;
-        i1 = min(cpt, i0 + per);
-        break;
-      }
-      before += x;
-    }
-    __syncthreads();
-    bool done = false;
-    for (int j0 = i0; j0 < i1 && !done; j0 += SAMPLE_STEPS) {
-      const int j1 = min(i1, j0 + SAMPLE_STEPS);
-      chunks(single{}, j0, j1, [&](int i, const float(&v)[EPC], int e0) {
-        const u64 x = wave_total(weight_of(v, e0));
-        if (lane == 0) sh.part[i - j0][wave] = x;
+    if (stage == 2) {
+      id_lim = found;
+    } else if (stage == 3) {
+      each_listed([&](float z, int e) {
+        if ((uint32_t)e == found) emit_drawn(z, e, total);
       });
-      __syncthreads();
-      for (int i = j0; i < j1 && !done; ++i)
-        for (int h = 0; h < NW && !done; ++h) {
-          const u64 x = sh.part[i - j0][h];
-          if (before + x <= want) {
-            before += x;
-            continue;
-          }
-          done = true;
-          if (h != wave) break;
-          chunks(single{}, i, i + 1, [&](int, const float(&v)[EPC], int e0) {
-            const u64 own = weight_of(v, e0);
-            u64 at = before + wave_upto(own) - own;
-#pragma unroll
-            for (int q = 0; q < EPC; ++q)
-              if (kept(v[q], e0 + q)) {
-                const u64 w = wt.units(v[q]);
-                if (at <= want && at + w > want) emit_drawn(v[q], e0 + q, total);
-                at += w;
-              }
-          });
-        }
-      __syncthreads();
+    } else if (reached) {
+      const float z = key_value(found);
+      const u64 one = max(wt.units(z), 1ull);
+      const u64 ties = stage == 0 ? k - c : (aim.want - w + one - 1) / one;
+      if (stage == 0) w_k = w + ties * wt.units(z);
+      if (z > cut.z)
+        cut = {z, ties};
+      else if (z == cut.z)  // the shorter of two prefixes
+        cut.ties = min(cut.ties, ties);
     }
   }
+  if (listed) return;
+
+  // the draw from the row: the part that the number falls into, then its run of chunks, the lane and the token
+  row.edges();
+  // weight of a chunk's kept logits (the one chunk in which the ties end is looked at closely)
+  const int last = (int)min(id_lim, 0x7FFFFFFFu);
+  const float least = cut.z, above = cut.z == -INFINITY ? cut.z : key_value(order_key(cut.z) + 1);
+  auto weight_of = [&](const float(&v)[EPC], int e0) {
+    const bool ends = e0 <= last && e0 + EPC - 1 > last;
+    const float bound = e0 > last ? above : least;
+    u64 x = 0;
+#pragma unroll
+    for (int q = 0; q < EPC; ++q) {
+      float z = v[q] >= bound ? v[q] : -INFINITY;
+      if (ends && !kept(v[q], e0 + q)) z = -INFINITY;
+      x += wt.biased(z);
+    }
+    return x - EPC * Weigher::BIAS;
+  };
+  const int gc = (row.nch + SAMPLE_GROUPS - 1) / SAMPLE_GROUPS, steps = (gc + 63) / 64;
+  auto group_chunks = [&](int g, int i0, int i1, auto f) {  // f(weight of the lane's chunk i, its logits, first id)
+    walk<2, 64>(row, g * gc + lane, i0, i1, [&](int i, int c, u32x4 w) {
+      float v[EPC];
+      unpack<T>(w, v);
+      const u64 x = weight_of(v, row.first(c));
+      f(i, c < (g + 1) * gc ? x : 0, v, row.first(c));
+    });
+  };
+  if (lim.any) {
+#pragma unroll 1
+    for (int g = wave; g < SAMPLE_GROUPS; g += NW) {
+      u64 x = 0;
+      group_chunks(g, 0, steps, [&](int, u64 y, const float(&)[EPC], int) { x += y; });
+      x = wave_total(x);
+      if (lane == 0) sh.part[g] = x;
+    }
+    __syncthreads();
+  } else if (threadIdx.x < SAMPLE_GROUPS) {
+    sh.part[threadIdx.x] = a.parts[slot * SAMPLE_GROUPS + threadIdx.x];
+  }
+  if (wave != 0) return;
+  // one wave from here: lane g has part g
+  const u64 mine = sh.part[lane], upto = wave_upto(mine);
+  total = last_lane(upto);
+  const u64 want = (u64)(u * (double)total);  // the first cumulative weight above it
+  const int g = __ffsll((unsigned long long)__ballot(upto > want)) - 1;
+  u64 before = (u64)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((upto - mine) >> 32), g) << 32 |
+               (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(upto - mine), g);
+  group_chunks(g, 0, steps, [&](int, u64 own, const float(&v)[EPC], int e0) {
+    const u64 sum = wave_upto(own);
+    if (before <= want && before + last_lane(sum) > want) {
+      u64 at = before + sum - own;
+#pragma unroll
+      for (int q = 0; q < EPC; ++q)
+        if (kept(v[q], e0 + q)) {
+          const u64 w = wt.units(v[q]);
+          if (own != 0 && at <= want && at + w > want) emit_drawn(v[q], e0 + q, total);
+          at += w;
+        }
+    }
+    before += last_lane(sum);
+  });
 }
 
 }  // namespace alr
