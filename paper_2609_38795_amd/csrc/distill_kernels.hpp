@@ -28,6 +28,7 @@ struct DistillArgs {
   float scale;
   long n;
   int V;
+  const float* w_sum;    // sum of the weights, or null: each workgroup forms it
   float* row_loss;       // [n]
   void* dz;              // rows of V, or unused
   long dz_rs;
@@ -82,7 +83,16 @@ __device__ __forceinline__ TailSum merge_tail(TailSum a, TailSum b) {
   return {m, a.s * fast_exp2((a.m - ref) * LOG2E) + b.s * fast_exp2((b.m - ref) * LOG2E)};
 }
 
-// One workgroup per row.  Each wave owns a run of `cpw` x 64 chunks of the row.
+__device__ __forceinline__ float lane_value(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+
+// One workgroup per row, which reads it for the sums and, with a gradient, again, mostly from the last-level
+// cache (keeping part of it in LDS or registers in between measured no faster).  What bounds it is HBM.  The running
+// maximum of the sums costs one exponential a chunk; they are formed while later loads are under way.
+//
+// Chunks that hold listed tokens (eight at most) are left out of both passes: lane j of every wave loads entry
+// j's chunk at the start, and the first wave's lanes take them at the end of each pass, all at once.
 template <typename T, int THREADS, bool GRAD>
 __global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
   constexpr int NW = THREADS / 64, EPC = RowChunks<T>::EPC;
@@ -91,13 +101,13 @@ __global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float inv_w = 0.f;
   if constexpr (GRAD) {
-    const double W = weight_sum(a.weight, a.n, red64);
+    const double W = a.w_sum ? (double)a.w_sum[0] : weight_sum(a.weight, a.n, red64);
     inv_w = W != 0.0 ? (float)((double)a.scale / W) : 0.f;
     if (a.up) inv_w *= a.up[0];
   }
   for (long r = blockIdx.x; r < a.n; r += gridDim.x) {
     RowChunks<T> row(static_cast<const T*>(a.z) + r * a.z_rs, a.V);
-    const int cpw = (row.nch + THREADS - 1) / THREADS;
+    const int cpt = (row.nch + THREADS - 1) / THREADS;  // chunk i of a thread: i * THREADS + its index
     T* dz = GRAD ? static_cast<T*>(a.dz) + r * a.dz_rs : nullptr;
     const bool vec =
         ((reinterpret_cast<uintptr_t>(dz) - (uintptr_t)row.mis * sizeof(T)) & 15) == 0;
@@ -106,51 +116,40 @@ __global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
       if (threadIdx.x == 0) a.row_loss[r] = 0.f;
       if constexpr (GRAD) {
         const float zero[EPC] = {};
-        for (int i = 0; i < cpw; ++i) {
-          const int c = (wave * cpw + i) * 64 + lane;
+        for (int i = 0; i < cpt; ++i) {
+          const int c = i * THREADS + (int)threadIdx.x;
           if (c < row.nch) store_chunk(row, dz, vec, c, zero);
         }
       }
       continue;
     }
     row.edges();
-    // the label; an id outside the vocabulary is passed over with its probability
-    int id[DISTILL_K];
-    float pi[DISTILL_K], zj[DISTILL_K];
-    bool first[DISTILL_K];
-    uint32_t hit = 0;  // bit i % 32: chunk i of this thread may hold a listed token
+    // The label: an id outside the vocabulary is passed over with its probability.  hit: bit i % 32 tells that
+    // chunk i of this thread may hold a listed token (is_hit, that it does).
+    int id[DISTILL_K], lane_id = -1;
+    uint32_t hit = 0;
 #pragma unroll
     for (int j = 0; j < DISTILL_K; ++j) {
       id[j] = a.ids[r * DISTILL_K + j];
-      const bool ok = id[j] >= 0 && id[j] < a.V;
-      if (!ok) id[j] = -1;
-      pi[j] = ok ? expf(a.logp[r * DISTILL_K + j]) : 0.f;
-      zj[j] = ok ? row.at(id[j]) : -INFINITY;
-      first[j] = ok;
-#pragma unroll
-      for (int k = 0; k < j; ++k)
-        if (id[k] == id[j]) first[j] = false;
-      const int c = (id[j] + row.mis) / EPC, g = c >> 6;
-      if (ok && (c & 63) == lane && g / cpw == wave) hit |= 1u << ((g - wave * cpw) & 31);
+      if (id[j] < 0 || id[j] >= a.V) id[j] = -1;
+      const int c = (id[j] + row.mis) / EPC;
+      if (id[j] >= 0 && c % THREADS == (int)threadIdx.x) hit |= 1u << (c / THREADS & 31);
+      if (lane == j) lane_id = id[j];
     }
+    const int lane_c = lane_id >= 0 ? (lane_id + row.mis) / EPC : 0;
+    const u32x4 lane_x = row.whole(lane_c, row.load(lane_c));
+    const float lane_lp = lane_id >= 0 ? a.logp[r * DISTILL_K + lane] : -INFINITY;
     const float tau = a.tail[r];
-    auto listed = [&](int e) {
+    auto is_hit = [&](int i, int c) {
+      if (!(hit >> (i & 31) & 1)) return false;
       bool in = false;
 #pragma unroll
-      for (int j = 0; j < DISTILL_K; ++j) in |= id[j] == e && e >= 0;
+      for (int j = 0; j < DISTILL_K; ++j) in |= id[j] >= 0 && (id[j] + row.mis) / EPC == c;
       return in;
     };
 
     TailSum t = {-INFINITY, 0.f};
-    for (int i = 0; i < cpw; ++i) {
-      const int c = (wave * cpw + i) * 64 + lane;
-      if (c >= row.nch) break;
-      float v[EPC];
-      unpack<T>(row.whole(c, row.load(c)), v);
-      if (hit >> (i & 31) & 1)
-#pragma unroll
-        for (int k = 0; k < EPC; ++k)
-          if (listed(row.first(c) + k)) v[k] = -INFINITY;
+    auto add_up = [&](const float(&v)[EPC]) {
       float m = t.m;
 #pragma unroll
       for (int k = 0; k < EPC; ++k) m = fmaxf(m, v[k]);
@@ -159,61 +158,90 @@ __global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
 #pragma unroll
       for (int k = 0; k < EPC; ++k) s += fast_exp2((v[k] - ref) * LOG2E);
       t = {m, s};
+    };
+    walk<4, THREADS>(row, (int)threadIdx.x, 0, cpt, [&](int i, int c, u32x4 x) {
+      float v[EPC];
+      unpack<T>(x, v);
+      if (!is_hit(i, c)) add_up(v);
+    });
+    // the entries, in the first eight lanes of each wave: their logits, which of a chunk's values are listed
+    // (in the first lane of each chunk), which is the first entry of its token
+    float lane_v[EPC], lane_z = -INFINITY;
+    unpack<T>(lane_x, lane_v);
+#pragma unroll
+    for (int k = 0; k < EPC; ++k)
+      if (lane_id >= 0 && row.first(lane_c) + k == lane_id) lane_z = lane_v[k];
+    uint32_t in = 0;
+    bool first_c = lane_id >= 0, first = first_c;
+#pragma unroll
+    for (int j = 0; j < DISTILL_K; ++j) {
+      if (id[j] < 0 || (id[j] + row.mis) / EPC != lane_c) continue;
+      in |= 1u << (id[j] + row.mis) % EPC;
+      if (j < lane) first_c = false;
+      if (j < lane && id[j] == lane_id) first = false;
+    }
+    if (wave == 0 && first_c) {
+      float v[EPC];
+#pragma unroll
+      for (int k = 0; k < EPC; ++k) v[k] = in >> k & 1 ? -INFINITY : lane_v[k];
+      add_up(v);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) t = merge_tail(t, TailSum{__shfl_xor(t.m, o), __shfl_xor(t.s, o)});
-    if (lane == 0) red[wave] = t;
-    __syncthreads();
-    t = red[0];
+    if constexpr (NW > 1) {
+      if (lane == 0) red[wave] = t;
+      __syncthreads();
+      t = red[0];
 #pragma unroll
-    for (int k = 1; k < NW; ++k) t = merge_tail(t, red[k]);
-    __syncthreads();  // red is written again for the next row
+      for (int k = 1; k < NW; ++k) t = merge_tail(t, red[k]);
+      __syncthreads();  // red is written again for the next row
+    }
 
-    float mx = t.m;
-#pragma unroll
-    for (int j = 0; j < DISTILL_K; ++j) mx = fmaxf(mx, first[j] ? zj[j] : -INFINITY);
+    const float lane_pi = expf(lane_lp);  // 0 where there is no entry
+    const float mx = fmaxf(t.m, wave_max(lane_z));
     const float ref = mx == -INFINITY ? 0.f : mx;
-    float s = t.s * expf(t.m - ref);
-#pragma unroll
-    for (int j = 0; j < DISTILL_K; ++j)
-      if (first[j]) s += expf(zj[j] - ref);
+    const float s = t.s * expf(t.m - ref) + lane_value(group_sum<8>(first ? expf(lane_z - ref) : 0.f), 0);
     const float ls = logf(s);
     const float lq_tail = (t.m - ref) + (logf(t.s) - ls);
-    float loss = tau > 0.f ? -tau * lq_tail : 0.f, mass = tau;
-#pragma unroll
-    for (int j = 0; j < DISTILL_K; ++j) {
-      if (pi[j] > 0.f) loss -= pi[j] * ((zj[j] - ref) - ls);
-      mass += pi[j];
-    }
+    const float terms = lane_pi > 0.f ? lane_pi * ((lane_z - ref) - ls) : 0.f;
+    const float loss = (tau > 0.f ? -tau * lq_tail : 0.f) - lane_value(group_sum<8>(terms), 0);
+    const float mass = tau + lane_value(group_sum<8>(lane_pi), 0);
     if (threadIdx.x == 0) a.row_loss[r] = loss;
     if constexpr (GRAD) {
       const float cw = inv_w * w;
       const float ref_t = t.m == -INFINITY ? 0.f : t.m;
       // no tail at all: every value outside the list is -inf and gets 0
       const float bt = t.s == 0.f ? 0.f : cw * (mass * expf(lq_tail) - tau) / t.s;
-      for (int i = 0; i < cpw; ++i) {
-        const int c = (wave * cpw + i) * 64 + lane;
-        if (c >= row.nch) break;
+      walk<4, THREADS>(row, (int)threadIdx.x, 0, cpt, [&](int i, int c, u32x4 x) {
+        if (c >= row.nch || is_hit(i, c)) return;
         float v[EPC];
-        unpack<T>(row.whole(c, row.load(c)), v);
-        float g[EPC];
+        unpack<T>(x, v);
 #pragma unroll
-        for (int k = 0; k < EPC; ++k) g[k] = bt * fast_exp2((v[k] - ref_t) * LOG2E);
-        if (hit >> (i & 31) & 1)
+        for (int k = 0; k < EPC; ++k) v[k] = bt * fast_exp2((v[k] - ref_t) * LOG2E);
+        store_chunk(row, dz, vec, c, v);
+      });
+      if (wave == 0) {
 #pragma unroll
-          for (int k = 0; k < EPC; ++k) {
-            const int e = row.first(c) + k;
-            if (!listed(e)) continue;
-            float d = mass * expf((v[k] - ref) - ls);
+        for (int k = 0; k < EPC; ++k) {
+          const int e = row.first(lane_c) + k;
+          float d = mass * expf((lane_v[k] - ref) - ls);
 #pragma unroll
-            for (int j = 0; j < DISTILL_K; ++j)
-              if (id[j] == e) d -= pi[j];
-            g[k] = cw * d;
-          }
-        store_chunk(row, dz, vec, c, g);
+          for (int j = 0; j < DISTILL_K; ++j)
+            if (id[j] == e) d -= lane_value(lane_pi, j);
+          lane_v[k] = in >> k & 1 ? cw * d : bt * fast_exp2((lane_v[k] - ref_t) * LOG2E);
+        }
+        if (first_c) store_chunk(row, dz, vec, lane_c, lane_v);
       }
     }
   }
+}
+
+// out[0] = sum of the weights, ahead of the gradients of many rows.
+__global__ __launch_bounds__(1024) void weight_sum_kernel(const float* __restrict__ w, long n,
+                                                          float* __restrict__ out) {
+  __shared__ double red[16];
+  const double W = weight_sum(w, n, red);
+  if (threadIdx.x == 0) out[0] = (float)W;
 }
 
 }  // namespace alr

@@ -990,14 +990,30 @@ void launch_qk_back(const alr_ctx* ctx, QkArgs a, float* dgq, float* dgk, hipStr
   qk_gain_grad_kernel<<<(2 * a.hd + 15) / 16, 1024, 0, st>>>(a.part, grid, a.hd, dgq, dgk);
 }
 
-template <typename T>
-void launch_distill(const DistillArgs& a, float* loss_out, hipStream_t st) {
+template <typename T, int THREADS>
+void launch_distill_rows(const DistillArgs& a, hipStream_t st) {
   const unsigned grid = (unsigned)std::min<long>(a.n, 1 << 20);
+  if (a.dz)
+    distill_rows_kernel<T, THREADS, true><<<grid, THREADS, 0, st>>>(a);
+  else
+    distill_rows_kernel<T, THREADS, false><<<grid, THREADS, 0, st>>>(a);
+}
+
+template <typename T>
+void launch_distill(DistillArgs a, float* loss_out, hipStream_t st) {
   if (a.n > 0) {
-    if (a.dz)
-      distill_rows_kernel<T, 256, true><<<grid, 256, 0, st>>>(a);
+    // a few weights each workgroup adds up itself; beyond, a launch ahead of them does
+    if (a.dz && a.weight && a.n > 256) {
+      weight_sum_kernel<<<1, 1024, 0, st>>>(a.weight, a.n, loss_out + 1);
+      a.w_sum = loss_out + 1;
+    }
+    const long chunks = ((long)a.V * (long)sizeof(T) + 15) / 16;
+    if (chunks <= 256)
+      launch_distill_rows<T, 64>(a, st);
+    else if (chunks <= 4096 || !a.dz)
+      launch_distill_rows<T, 256>(a, st);
     else
-      distill_rows_kernel<T, 256, false><<<grid, 256, 0, st>>>(a);
+      launch_distill_rows<T, 512>(a, st);
   }
   distill_reduce_kernel<<<1, 1024, 0, st>>>(a.row_loss, a.weight, a.n, a.scale, loss_out);
 }
