@@ -238,6 +238,10 @@ class Engine:
             raise AlrError(st or 1, buf.value.decode() or "invalid limits")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self.ws_bytes = nbytes
+        self._index = self.workspace.get_device()
+        self._f32, self._i32 = (torch.float32,), (torch.int32,)
+        self._logit_types = (torch.bfloat16, torch.float32)
+        self._own_type = (torch.bfloat16 if shape.dtype == "bf16" else torch.float32,)
         dev_w = self._upload_weights(weights)
         w = AlrWeights()
         keep = []
@@ -451,17 +455,18 @@ class Engine:
         """Checks a device tensor argument (the library sees only its address): on this
         context's device, of the shape and a dtype asked for, contiguous, or, `strided`, rows of
         contiguous values at any row stride."""
-        if t.device != self.workspace.device:
+        if t.get_device() != self._index:
             raise ValueError(f"{name}: on {t.device}, the context is on {self.workspace.device}")
-        if tuple(t.shape) != tuple(shape):
+        if t.shape != shape:
             raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
         if t.dtype not in dtypes:
             raise ValueError(f"{name}: dtype {t.dtype}, expected {' or '.join(map(str, dtypes))}")
-        if strided:
-            if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        if not t.is_contiguous():
+            if not strided:
+                raise ValueError(f"{name}: must be contiguous")
+            (rows, cols), (rs, cs) = shape, t.stride()
+            if cols > 1 and cs != 1 or rows > 1 and rs < cols:
                 raise ValueError(f"{name}: rows must be contiguous and must not overlap")
-        elif not t.is_contiguous():
-            raise ValueError(f"{name}: must be contiguous")
         return t.data_ptr()
 
     @staticmethod
@@ -476,11 +481,10 @@ class Engine:
         if temperature is None and top_k is None and top_p is None and min_p is None:
             return None
         sp = AlrSampling()
-        for name, t, dt in (("temperature", temperature, torch.float32),
-                            ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
-                            ("min_p", min_p, torch.float32)):
+        for name, t, dt in (("temperature", temperature, self._f32), ("top_k", top_k, self._i32),
+                            ("top_p", top_p, self._f32), ("min_p", min_p, self._f32)):
             if t is not None:
-                setattr(sp, name, self._tensor(name, t, (n,), (dt,)))
+                setattr(sp, name, self._tensor(name, t, (n,), dt))
         return ctypes.byref(sp)
 
     def sample(self, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None,
@@ -490,17 +494,17 @@ class Engine:
         log-probs fp32 [n] of the draws), into ``out`` if given (its second entry may be None)."""
         torch = self.torch
         n, V = logits.shape
-        lp = self._tensor("logits", logits, (n, V), (torch.bfloat16, torch.float32), strided=True)
+        lp = self._tensor("logits", logits, (n, V), self._logit_types, strided=True)
         sp = self._sampling(n, temperature, top_k, top_p, min_p)
-        up = self._tensor("uniform", uniform, (n,), (torch.float32,))
+        up = self._tensor("uniform", uniform, (n,), self._f32)
         if out is None:
             out = (torch.empty(n, dtype=torch.int32, device=self.device),
                    torch.empty(n, dtype=torch.float32, device=self.device))
         tok, logp = out
         st = self.lib.alr_sample(
             self.ctx, n, V, lp, self._dtype_code(logits), self._row_stride(logits), sp, up,
-            self._tensor("tokens", tok, (n,), (torch.int32,)),
-            None if logp is None else self._tensor("logp", logp, (n,), (torch.float32,)),
+            self._tensor("tokens", tok, (n,), self._i32),
+            None if logp is None else self._tensor("logp", logp, (n,), self._f32),
             self._sp())
         if st != 0:
             self._err(st)
@@ -528,7 +532,7 @@ class Engine:
         st = self.lib.alr_rollout_sampled(
             self.ctx, n, _i32p(a_s), _i32p(a_p), block,
             self._sampling(n, temperature, top_k, top_p, min_p),
-            self._tensor("uniform", uniform, (n, block), (torch.float32,)), ptr(forced),
+            self._tensor("uniform", uniform, (n, block), self._f32), ptr(forced),
             *(ptr(t) for t in out), self._sp())
         if st != 0:
             self._err(st)
@@ -544,8 +548,8 @@ class Engine:
         torch = self.torch
         n, V = logits.shape
         f32 = (torch.float32,)
-        lp = self._tensor("logits", logits, (n, V), (torch.bfloat16, torch.float32), strided=True)
-        label = [self._tensor("top_ids", top_ids.reshape(-1, ALR_TOPK), (n, ALR_TOPK), (torch.int32,)),
+        lp = self._tensor("logits", logits, (n, V), self._logit_types, strided=True)
+        label = [self._tensor("top_ids", top_ids.reshape(-1, ALR_TOPK), (n, ALR_TOPK), self._i32),
                  self._tensor("top_logp", top_logp.reshape(-1, ALR_TOPK), (n, ALR_TOPK), f32),
                  self._tensor("tail", tail.reshape(-1), (n,), f32),
                  None if weight is None else self._tensor("weight", weight.reshape(-1), (n,), f32)]
@@ -572,10 +576,9 @@ class Engine:
         if t is None:
             return 0, None, 0
         hd = self.shape.head_dim
-        dt = torch.bfloat16 if self.shape.dtype == "bf16" else torch.float32
         if t.dim() != 2 or t.shape[1] % hd or t.shape[1] == 0:
             raise ValueError(f"{name}: shape {tuple(t.shape)} is no rows of {hd}-value heads")
-        return (t.shape[1] // hd, self._tensor(name, t, (n, t.shape[1]), (dt,), strided=True),
+        return (t.shape[1] // hd, self._tensor(name, t, (n, t.shape[1]), self._own_type, strided=True),
                 self._row_stride(t))
 
     def qk_norm_rope(self, q, k, q_gain, k_gain, positions=None, out=None):
@@ -615,7 +618,7 @@ class Engine:
         outs = self._heads("dq", out[0], n), self._heads("dk", out[1], n)
         if any((a[0], b[0]) != (H, G) for a, b in (ins, outs)):
             raise ValueError("gradients must have the heads of q and k")
-        gain = [None if t is None else self._tensor(nm, t, (hd,), (torch.float32,))
+        gain = [None if t is None else self._tensor(nm, t, (hd,), self._f32)
                 for nm, t in (("dq_gain", out[2]), ("dk_gain", out[3]))]
         st = self.lib.alr_qk_norm_rope_backward(
             self.ctx, n, H, G, self._positions(positions, n), qp, qs, kp, ks,
@@ -634,8 +637,7 @@ class Engine:
         torch = self.torch
         if heads == 0:
             return None
-        dt = torch.bfloat16 if self.shape.dtype == "bf16" else torch.float32
-        return self._tensor(name, g, (self.shape.head_dim,), (dt,))
+        return self._tensor(name, g, (self.shape.head_dim,), self._own_type)
 
     def set_qk_norm(self, q_gain=None, k_gain=None):
         """alr_set_qk_norm: per-layer gains [head_dim] (numpy, as the other weights) that turn the

@@ -65,7 +65,7 @@ struct Layout {
   size_t part_o, part_ml;
   size_t splitk, splitk_bytes;
   size_t qk_part;
-  size_t sample_rows, sample_hdr, sample_list, sample_seg, sample_part;
+  size_t sample_rows, sample_hdr, sample_list, sample_seg, sample_part, sample_slow;
   size_t max_pwork, max_dwork, max_groups;
   size_t total;
 };
@@ -280,6 +280,7 @@ size_t compute_layout(const alr_config& c, const alr_limits& lim, Layout& L) {
   L.sample_list = take(L.sample_rows * SAMPLE_LIST * sizeof(f32x2));
   L.sample_seg = take(L.sample_rows * SAMPLE_SEGS * sizeof(SampleSeg));
   L.sample_part = take(L.sample_rows * SAMPLE_GROUPS * 8);
+  L.sample_slow = take((1 + L.sample_rows) * 4);
   // gain gradients of the q/k norms, one partial sum a workgroup
   L.qk_part = take((size_t)QK_BACK_WGS * 2 * hd * 4);
   L.total = off;
@@ -1270,6 +1271,7 @@ void launch_sample(const alr_ctx* ctx, SampleArgs a, hipStream_t st) {
   a.lists = ctx->at<f32x2>(L.sample_list);
   a.segs = ctx->at<SampleSeg>(L.sample_seg);
   a.parts = ctx->at<unsigned long long>(L.sample_part);
+  a.slow = ctx->at<uint32_t>(L.sample_slow);
   for (a.row0 = 0; a.row0 < n; a.row0 += cap) {
     a.n = std::min(cap, n - a.row0);
     // segments of at least two chunks a thread, 16 workgroups per CU where there are that many
@@ -1280,10 +1282,8 @@ void launch_sample(const alr_ctx* ctx, SampleArgs a, hipStream_t st) {
     const unsigned grid = (unsigned)(a.n * a.n_seg);
     sample_scan_kernel<T, true><<<grid, 256, 0, st>>>(a);
     sample_scan_kernel<T, false><<<grid, 256, 0, st>>>(a);
-    if (a.n <= ctx->n_cu)
-      sample_settle_kernel<T, 1024><<<(unsigned)a.n, 1024, 0, st>>>(a);
-    else
-      sample_settle_kernel<T, 512><<<(unsigned)a.n, 512, 0, st>>>(a);
+    sample_settle_kernel<T, 512, false><<<(unsigned)a.n, 512, 0, st>>>(a);
+    sample_settle_kernel<T, 1024, true><<<(unsigned)a.n, 1024, 0, st>>>(a);
   }
 }
 

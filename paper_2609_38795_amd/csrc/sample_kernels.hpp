@@ -43,6 +43,7 @@ struct SampleArgs {
   f32x2* lists;           // [cap, SAMPLE_LIST]
   struct SampleSeg* segs; // [cap, SAMPLE_SEGS]
   unsigned long long* parts;  // [cap, SAMPLE_GROUPS]
+  uint32_t* slow;         // [1 + cap]: how many rows their list does not settle, and which
   long row0;
   int n_seg;              // segments of a row, each a workgroup's, in the scans
 };
@@ -189,10 +190,11 @@ struct Weigher {
   __device__ __forceinline__ double log2_of(float z) const { return ((double)z - m) * c * (1.0 / 32); }
 };
 
-struct SampleShared {
+template <int LEVELS>
+struct SampleSharedOf {
   double tab[32];
-  uint32_t cnt[2][SAMPLE_BINS];  // of the first level over a row, of the narrowing ones
-  u64 mass[2][SAMPLE_BINS];
+  uint32_t cnt[LEVELS][SAMPLE_BINS];  // of the narrowing levels; of the first one, over a row
+  u64 mass[LEVELS][SAMPLE_BINS];
   f32x2 list[SAMPLE_LIST];       // (logit, id) of the logits set aside, a run of it per wave
   uint32_t scan_c[16], few_n;
   u64 scan_m[16];
@@ -206,8 +208,8 @@ struct SampleShared {
 };
 
 // min and max of unsigned values over the workgroup
-template <int NW>
-__device__ __forceinline__ void block_range(uint32_t& lo, uint32_t& hi, SampleShared& sh) {
+template <int NW, typename S>
+__device__ __forceinline__ void block_range(uint32_t& lo, uint32_t& hi, S& sh) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     lo = min(lo, (uint32_t)__shfl_xor(lo, o));
@@ -227,8 +229,8 @@ __device__ __forceinline__ void block_range(uint32_t& lo, uint32_t& hi, SampleSh
 }
 
 // a count and a sum of weights over the workgroup
-template <int NW>
-__device__ __forceinline__ void block_sums(uint32_t& c, u64& m, SampleShared& sh) {
+template <int NW, typename S>
+__device__ __forceinline__ void block_sums(uint32_t& c, u64& m, S& sh) {
   c = wave_total(c);
   m = wave_total(m);
   if ((threadIdx.x & 63) == 0) {
@@ -246,8 +248,8 @@ __device__ __forceinline__ void block_sums(uint32_t& c, u64& m, SampleShared& sh
   __syncthreads();
 }
 
-template <int THREADS>
-__device__ __forceinline__ void clear_bins(SampleShared& sh, int level) {
+template <int THREADS, typename S>
+__device__ __forceinline__ void clear_bins(S& sh, int level) {
 #pragma unroll
   for (int b = threadIdx.x; b < SAMPLE_BINS; b += THREADS) {
     sh.cnt[level][b] = 0;
@@ -266,8 +268,8 @@ struct Aim {
 // Finds the aim's bin; above_c and above_m come in as what lies before the level's bins and go out as
 // what lies before the bin.  Returns -1 where the bins do not reach it.  mass_of(total weight of
 // the bins) may still set the aim (a share of a whole that only the bins know).
-template <int THREADS, typename F>
-__device__ __forceinline__ int find_bin(SampleShared& sh, int level, Aim& aim, uint32_t& above_c,
+template <int THREADS, typename S, typename F>
+__device__ __forceinline__ int find_bin(S& sh, int level, Aim& aim, uint32_t& above_c,
                                         u64& above_m, F mass_of) {
   constexpr int NW = THREADS / 64, PER = SAMPLE_BINS / THREADS;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b0 = threadIdx.x * PER;
@@ -328,26 +330,26 @@ __device__ __forceinline__ int find_bin(SampleShared& sh, int level, Aim& aim, u
 // above_c and above_m come in as what lies before hi (lo) and end as what lies before that key.  A level
 // of bins over the keys' range leaves few values as a rule, which are ranked against each other; else another
 // level splits the bin.  False where the values do not reach the aim.
-template <int THREADS, typename E>
-__device__ __forceinline__ bool pick(SampleShared& sh, const Weigher& wt, bool up, Aim aim, uint32_t lo,
+template <int THREADS, typename S, typename E>
+__device__ __forceinline__ bool pick(S& sh, const Weigher& wt, bool up, Aim aim, uint32_t lo,
                                      uint32_t hi, uint32_t& above_c, u64& above_m, uint32_t& found,
                                      E each) {
   while (true) {
     const uint32_t range = hi - lo;
     const int shift = range ? max(0, 32 - SAMPLE_BITS - (int)__clz(range)) : 0;  // range >> shift: a bin
     if (threadIdx.x == 0) sh.few_n = 0;
-    clear_bins<THREADS>(sh, 1);
+    clear_bins<THREADS>(sh, 0);
     each([&](uint32_t key, float z) {
       if (key >= lo && key <= hi) {
         const uint32_t b = (up ? key - lo : hi - key) >> shift;
-        atomicAdd(&sh.cnt[1][b], 1u);
-        atomicAdd(&sh.mass[1][b], wt.units(z));
+        atomicAdd(&sh.cnt[0][b], 1u);
+        atomicAdd(&sh.mass[0][b], wt.units(z));
       }
     });
     __syncthreads();
-    const int b = find_bin<THREADS>(sh, 1, aim, above_c, above_m, [](u64) {});
+    const int b = find_bin<THREADS>(sh, 0, aim, above_c, above_m, [](u64) {});
     if (b < 0) return false;
-    const uint32_t width = (1u << shift) - 1, n = sh.cnt[1][b];
+    const uint32_t width = (1u << shift) - 1, n = sh.cnt[0][b];
     if (up) {
       lo += (uint32_t)b << shift;
       hi = min(hi, lo + min(0xFFFFFFFFu - lo, width));
@@ -635,6 +637,7 @@ __global__ __launch_bounds__(256, 4) void sample_scan_kernel(SampleArgs a) {
   if constexpr (FIRST) {
     s = scan_max(row, a.n_seg, seg, sh.red);
     if (threadIdx.x != 0) return;
+    if (blockIdx.x == 0) a.slow[0] = 0;
     if (seg == 0) {
       a.rows[slot].whole = 0;
       a.rows[slot].n_list = 0;
@@ -656,16 +659,19 @@ __global__ __launch_bounds__(256, 4) void sample_scan_kernel(SampleArgs a) {
 }
 
 // Settles a row from what the scans left.  Limits that fall within the list are settled there, and so is the
-// draw.  Others (a nucleus of a flat distribution, a k of thousands) take a histogram of the row, the list
-// becomes that of the bin they fall into, and the draw reads the row again.  Without limits only the part of
-// the row that the number falls into is read again.
-template <typename T, int THREADS>
+// draw; without limits the part of the row that the number falls into is read again.  What bounds it is the
+// chain of picks, each some eight barriers long.  Rows whose list falls short (a nucleus of a flat distribution,
+// a k of thousands) are left to the SLOW form, a launch of its own, whose workgroups have a CU to themselves:
+// a histogram of the row, the list becomes that of the bin the limit falls into, and the draw reads the row again.
+template <typename T, int THREADS, bool SLOW>
 __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a) {
   constexpr int NW = THREADS / 64, EPC = RowChunks<T>::EPC, RUN = SAMPLE_LIST / NW;
   static_assert(SAMPLE_BINS % THREADS == 0 && NW <= 16, "bins per thread");
-  __shared__ SampleShared sh;
+  __shared__ SampleSharedOf<SLOW ? 2 : 1> sh;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long slot = dealt_row(blockIdx.x, a.n), r = a.row0 + slot;
+  // (in the order of the list, so that no workgroup with work waits behind one in a row of empty ones)
+  if (SLOW && blockIdx.x >= a.slow[0]) return;
+  const long slot = SLOW ? (long)a.slow[1 + blockIdx.x] : dealt_row(blockIdx.x, a.n), r = a.row0 + slot;
   const long idx = a.perm ? (long)a.perm[r] : r, o = idx * a.block + a.s;
   auto emit = [&](int tok, float lp) {
     a.tokens[o] = tok;
@@ -677,6 +683,9 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
   };
   const SampleRow hdr = a.rows[slot];
   const float m = hdr.m, line = hdr.line;
+  auto leave_to_slow = [&]() {
+    if (threadIdx.x == 0) a.slow[1 + atomicAdd(a.slow, 1u)] = (uint32_t)slot;
+  };
   if (m == -INFINITY) {  // nothing to draw
     if (threadIdx.x == 0) emit(-1, -INFINITY);
     return;
@@ -747,18 +756,18 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
   auto bin0 = [&](float z) { return (int)fminf((m - z) * cs, (float)(SAMPLE_BINS - 1)); };
   bool binned = false;
   auto bin_row = [&]() {
-    clear_bins<THREADS>(sh, 0);
+    clear_bins<THREADS>(sh, 1);
     if (by_p)
       each(heavy{}, [&](float z, int) {
         if (real(z)) {
           const int q = bin0(z);
-          if (by_k) atomicAdd(&sh.cnt[0][q], 1u);
-          atomicAdd(&sh.mass[0][q], wt.units(z));
+          if (by_k) atomicAdd(&sh.cnt[1][q], 1u);
+          atomicAdd(&sh.mass[1][q], wt.units(z));
         }
       });
     else
       each(light{}, [&](float z, int) {
-        if (real(z)) atomicAdd(&sh.cnt[0][bin0(z)], 1u);
+        if (real(z)) atomicAdd(&sh.cnt[1][bin0(z)], 1u);
       });
     __syncthreads();
     binned = true;
@@ -768,8 +777,12 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
   // what is not listed is not kept: the list is the row, or ends where min_p does
   const bool all = line == -INFINITY || (!lim.below_counts() && cut.z >= line);
   // listed: every logit that may be kept is in the list (and the limits are settled there)
-  bool listed = lim.any && fits && (by_k ? hdr.n_list >= k || all : by_p || all);
-  if (listed) {
+  bool listed = !SLOW && lim.any && fits && (by_k ? hdr.n_list >= k || all : by_p || all);
+  if (!SLOW && lim.any && !listed) {
+    leave_to_slow();
+    return;
+  }
+  if (!SLOW && listed) {
     n_list = hdr.n_list;
     for (uint32_t i = threadIdx.x; i < n_list; i += THREADS)
       aside.run[i / THREADS * 64 + lane] = a.lists[slot * SAMPLE_LIST + i];
@@ -777,6 +790,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
     aside.mine = n_list / THREADS * 64 + (rest > skip ? min(rest - skip, 64u) : 0);
   }
   u64 w_k = hdr.whole, total = 0;  // weight of the first k, or of all; of the kept
+  if (SLOW) row.edges();
 
   // The limits, ties and the draw, one after the other, each the pick of a value among ranked ones: of a
   // logit by count (k) or by weight (p), of an id by count (ties at the cut) or by weight (the draw).
@@ -794,12 +808,12 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
     if (stage == 1 && !by_p) continue;
     if (stage == 2) {
       if (cut.ties == ALL_TIES) continue;
-      if (!listed) from_list = bin_listed >= 0 && bin_listed == bin0(cut.z);
+      if (SLOW) from_list = bin_listed >= 0 && bin_listed == bin0(cut.z);
       from = upto = cut.z;
       aim.want = cut.ties;
     }
     if (stage == 3) {
-      if (!listed) break;
+      if (SLOW) break;
       from = cut.z;
       to_id = id_lim;
     }
@@ -817,12 +831,11 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
         if (real(z) && z >= from && z <= upto) f(up ? (uint32_t)e : order_key(z), z);
       });
     };
-    if (!listed) row.edges();
-    if (!up && !listed) {
+    if (SLOW && !up) {
       // narrowed to a bin of the row, whose logits become the list
       if (!binned) bin_row();
       if (stage == 1) aim.want = share_of(w_k);
-      const int bin = find_bin<THREADS>(sh, 0, aim, c, w, [&](u64 sum) {
+      const int bin = find_bin<THREADS>(sh, 1, aim, c, w, [&](u64 sum) {
         if (stage == 0) w_k = sum;
       });
       if (bin < 0) continue;  // fewer than k can be drawn
@@ -853,7 +866,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
         }
         aim.want = share_of(w_k);
       } else if (stage == 2) {
-        if (from_list)
+        if (!SLOW || from_list)
           visit([&](uint32_t, float) { ++here; });
         else
           visit_row([&](uint32_t, float) { ++here; });
@@ -875,12 +888,14 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
         block_range<NW>(lo, hi, sh);
       }
     }
-    const bool reached = from_list ? pick<THREADS>(sh, wt, up, aim, lo, hi, c, w, found, visit)
-                                   : pick<THREADS>(sh, wt, up, aim, lo, hi, c, w, found, visit_row);
-    if (!reached && stage == 1 && !all) {  // the list ends before top_p does
-      listed = false;
-      --stage;
-      continue;
+    bool reached;
+    if (!SLOW || from_list)
+      reached = pick<THREADS>(sh, wt, up, aim, lo, hi, c, w, found, visit);
+    else
+      reached = pick<THREADS>(sh, wt, up, aim, lo, hi, c, w, found, visit_row);
+    if (!SLOW && !reached && stage == 1 && !all) {  // the list ends before top_p does
+      leave_to_slow();
+      return;
     }
     if (stage == 2) {
       id_lim = found;
@@ -899,10 +914,10 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
         cut.ties = min(cut.ties, ties);
     }
   }
-  if (listed) return;
+  if (!SLOW && lim.any) return;
 
   // the draw from the row: the part that the number falls into, then its run of chunks, the lane and the token
-  row.edges();
+  if (!SLOW) row.edges();
   // weight of a chunk's kept logits (the one chunk in which the ties end is looked at closely)
   const int last = (int)min(id_lim, 0x7FFFFFFFu);
   const float least = cut.z, above = cut.z == -INFINITY ? cut.z : key_value(order_key(cut.z) + 1);
@@ -927,7 +942,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
       f(i, c < (g + 1) * gc ? x : 0, v, row.first(c));
     });
   };
-  if (lim.any) {
+  if (SLOW) {
 #pragma unroll 1
     for (int g = wave; g < SAMPLE_GROUPS; g += NW) {
       u64 x = 0;
