@@ -385,8 +385,8 @@ typedef struct {
  *   logp_out    DEVICE fp32 [n] or NULL: log of the probability with which the
  *               token was drawn, its share of the kept weight (0 for a greedy row).
  * Weights are formed in 64 bits and rounded to 2^-43 or less of the largest, so
- * their sums are exact: what a row gives depends on that row alone.  n = 0 is a
- * no-op. */
+ * their sums are exact: what a row gives depends on that row alone.  Uses the
+ * context's workspace.  n = 0 is a no-op. */
 alr_status alr_sample(alr_ctx* ctx, int32_t n, int32_t vocab, const void* logits, int32_t dtype,
                       int64_t row_stride, const alr_sampling* sampling, const float* uniform,
                       int32_t* tokens_out, float* logp_out, alr_stream stream);
@@ -456,7 +456,8 @@ alr_status alr_distill_loss(alr_ctx* ctx, int32_t n, int32_t vocab, const void* 
  *   q, k        DEVICE, row r at r * stride elements, its heads next to each other
  *               (so q and k may be column ranges of one projection's output).
  *   q_gain, k_gain  DEVICE [head_dim].
- *   q_out, k_out  DEVICE rows as q and k; may be q and k themselves.
+ *   q_out, k_out  DEVICE rows as q and k; may be q and k themselves (same strides), else
+ *               must not overlap them.
  * Arguments of a kind without heads are not looked at.  n = 0 is a no-op. */
 alr_status alr_qk_norm_rope(alr_ctx* ctx, int32_t n, int32_t q_heads, int32_t k_heads,
                             const int32_t* positions, const void* q, int64_t q_stride,
@@ -465,7 +466,8 @@ alr_status alr_qk_norm_rope(alr_ctx* ctx, int32_t n, int32_t q_heads, int32_t k_
                             int64_t k_out_stride, alr_stream stream);
 
 /* Gradients of alr_qk_norm_rope: from its inputs and the gradients of its outputs
- * (dq_out, dk_out) those of q and k (dq, dk; may be dq_out and dk_out themselves) and of the gains,
+ * (dq_out, dk_out) those of q and k (dq, dk; may be dq_out and dk_out, or q and k, themselves, with
+ * their strides, else must not overlap them) and of the gains,
  * summed over rows and heads in fp32 in a fixed order (dq_gain, dk_gain: DEVICE fp32
  * [head_dim]; 0 for n = 0).  Uses the context's workspace. */
 alr_status alr_qk_norm_rope_backward(alr_ctx* ctx, int32_t n, int32_t q_heads, int32_t k_heads,

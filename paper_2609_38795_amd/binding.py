@@ -477,7 +477,6 @@ class Engine:
         return ALR_BF16 if t.dtype == self.torch.bfloat16 else ALR_F32
 
     def _sampling(self, n, temperature, top_k, top_p, min_p):
-        torch = self.torch
         if temperature is None and top_k is None and top_p is None and min_p is None:
             return None
         sp = AlrSampling()
@@ -528,12 +527,17 @@ class Engine:
                    torch.empty((n, block, self.shape.vocab), **f32) if want_logprobs else None,
                    torch.empty((n, block, self.shape.n_feat, self.shape.d_model), **f32)
                    if want_feats and self.shape.n_feat > 0 else None)
-        ptr = (lambda t: None if t is None else t.data_ptr())
+        checked = (lambda name, t, dtypes, *tail: None if t is None else
+                   self._tensor(name, t, (n, block) + tail, dtypes))
+        tok, tok_lp, ids, lps, tl, rows, feats = out
         st = self.lib.alr_rollout_sampled(
             self.ctx, n, _i32p(a_s), _i32p(a_p), block,
             self._sampling(n, temperature, top_k, top_p, min_p),
-            self._tensor("uniform", uniform, (n, block), self._f32), ptr(forced),
-            *(ptr(t) for t in out), self._sp())
+            checked("uniform", uniform, self._f32), checked("forced", forced, self._i32),
+            checked("tokens", tok, self._i32), checked("token_logp", tok_lp, self._f32),
+            checked("top_ids", ids, self._i32, ALR_TOPK), checked("top_logp", lps, self._f32, ALR_TOPK),
+            checked("tail", tl, self._f32), checked("logprobs", rows, self._f32, self.shape.vocab),
+            checked("feats", feats, self._f32, self.shape.n_feat, self.shape.d_model), self._sp())
         if st != 0:
             self._err(st)
         return out

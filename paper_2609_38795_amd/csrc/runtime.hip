@@ -2371,6 +2371,15 @@ alr_status check_heads(alr_ctx* ctx, const char* name, int32_t heads, const void
   return ALR_OK;
 }
 
+// Rows may be replaced in place, each by its own result.
+alr_status check_in_place(alr_ctx* ctx, const char* name, int32_t n, int32_t heads, const void* in,
+                          int64_t in_stride, const void* out, int64_t out_stride) {
+  if (heads > 0 && n > 1 && in == out && in_stride != out_stride)
+    return fail(ctx, ALR_E_INVALID_ARG, "%s in place needs the row stride %lld, not %lld", name,
+                (long long)in_stride, (long long)out_stride);
+  return ALR_OK;
+}
+
 alr_status check_qk(alr_ctx* ctx, int32_t n, int32_t q_heads, int32_t k_heads,
                     const int32_t* positions) {
   if (n < 0 || q_heads < 0 || k_heads < 0 || q_heads + (int64_t)k_heads < 1 ||
@@ -2398,6 +2407,8 @@ alr_status alr_qk_norm_rope(alr_ctx* ctx, int32_t n, int32_t q_heads, int32_t k_
   const int64_t qs[] = {q_stride, q_out_stride}, ks[] = {k_stride, k_out_stride};
   st = check_heads(ctx, "q", q_heads, qp, 3, qs, 2);
   if (st == ALR_OK) st = check_heads(ctx, "k", k_heads, kp, 3, ks, 2);
+  if (st == ALR_OK) st = check_in_place(ctx, "q", n, q_heads, q, q_stride, q_out, q_out_stride);
+  if (st == ALR_OK) st = check_in_place(ctx, "k", n, k_heads, k, k_stride, k_out, k_out_stride);
   if (st != ALR_OK) return st;
   QkArgs a = qk_args(ctx, n, q_heads, k_heads);
   a.q = q;
@@ -2439,6 +2450,12 @@ alr_status alr_qk_norm_rope_backward(alr_ctx* ctx, int32_t n, int32_t q_heads, i
     const int64_t ks[] = {k_stride, dk_out_stride, dk_stride};
     st = check_heads(ctx, "q", q_heads, qp, 4, qs, 3);
     if (st == ALR_OK) st = check_heads(ctx, "k", k_heads, kp, 4, ks, 3);
+    if (st == ALR_OK)
+      st = check_in_place(ctx, "dq", n, q_heads, dq_out, dq_out_stride, dq, dq_stride);
+    if (st == ALR_OK)
+      st = check_in_place(ctx, "dk", n, k_heads, dk_out, dk_out_stride, dk, dk_stride);
+    if (st == ALR_OK) st = check_in_place(ctx, "dq", n, q_heads, q, q_stride, dq, dq_stride);
+    if (st == ALR_OK) st = check_in_place(ctx, "dk", n, k_heads, k, k_stride, dk, dk_stride);
     if (st != ALR_OK) return st;
   }
   QkArgs a = qk_args(ctx, n, q_heads, k_heads);

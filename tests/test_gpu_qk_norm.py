@@ -192,6 +192,44 @@ def test_captured_replays_and_another_stream():
     eng.close()
 
 
+def test_in_place_needs_the_same_row_stride():
+    """A row written at another stride would land on rows that are still read."""
+    hd, n = 64, 5
+    eng = engine("bf16", 4, 4, hd, 16)
+    x = torch.zeros(n, 512, dtype=torch.bfloat16, device="cuda")
+    g, dg = torch.ones(hd, dtype=torch.bfloat16, device="cuda"), torch.zeros(hd, device="cuda")
+    y = torch.zeros_like(x)
+    a, b, gp, dgp, lib, ctx, s = x.data_ptr(), y.data_ptr(), g.data_ptr(), dg.data_ptr(), eng.lib, eng.ctx, eng._sp()
+
+    def fwd(rows, out_stride):
+        return lib.alr_qk_norm_rope(ctx, rows, 4, 0, None, a, 512, None, 0, gp, None, a, out_stride, None, 0, s)
+
+    def back(rows, dy, dx, stride):
+        return lib.alr_qk_norm_rope_backward(ctx, rows, 4, 0, None, a, 512, None, 0, gp, None, dy, 512, None, 0,
+                                             dx, stride, None, 0, dgp, None, s)
+
+    assert fwd(n, 256) == 1 and b"in place" in lib.alr_last_error(ctx)
+    assert back(n, b, b, 256) == 1 and back(n, b, a, 256) == 1
+    assert fwd(n, 512) == 0 and fwd(1, 256) == 0 and back(n, b, b, 512) == 0 and back(n, b, a, 512) == 0
+    torch.cuda.synchronize()
+    eng.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_in_the_inputs_place(dtype):
+    n, H, G, hd = 37, 6, 2, 128
+    eng = engine(dtype, 8, 2, hd, 64)
+    q, k, gq, gk, pos, _ = make(n, H, G, hd, dtype, 3, 64)
+    p = torch.from_numpy(pos).cuda()
+    dq, dk = torch.randn(q.shape, device="cuda").to(q.dtype), torch.randn(k.shape, device="cuda").to(k.dtype)
+    ref = eng.qk_norm_rope_backward(q, k, gq, gk, dq, dk, positions=p)
+    dg = [torch.empty(hd, device="cuda") for _ in range(2)]
+    got = eng.qk_norm_rope_backward(q, k, gq, gk, dq, dk, positions=p, out=(q, k, *dg))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, ref))
+    eng.close()
+
+
 def test_refusals():
     hd = 64
     eng = engine("bf16", 4, 4, hd, 16)
