@@ -6,9 +6,14 @@
 // the first, in the order of the ids, whose cumulative kept weight exceeds u times the total.
 //
 // Each of those prefixes is "logits above a cut, and the first few ids at the cut", so no row is
-// sorted: a histogram over (max - z) finds the interval of logits that the k-th token, or the p-th of
-// the weight, falls into, histograms over the bits of the logits narrow it to one value, and a scan
-// over the ids settles the ties.
+// sorted: the cut, the ties at it and the token are each the pick of one value among ranked ones.
+//
+// Four launches.  Two scans, by up to 16 workgroups a row so that few rows fill the card too: the
+// first takes the maximum and, from the maxima of a thousand parts, a line above which a few thousand
+// logits lie; the second sets those aside, and adds up the row's weight where top_p is of the whole
+// row.  A third settles every row whose limits fall within its list, a fourth the others, from
+// histograms of the row.  (One launch that did it all spilled 64-bit registers, left one workgroup
+// to a CU and took twice as long.)
 //
 // Weights are whole numbers of 2^-shift (shift >= 43), from 64-bit exponentials, so every sum is exact
 // and does not depend on the order in which it is formed: what a row gives depends on its own values
@@ -123,32 +128,6 @@ __device__ __forceinline__ uint32_t order_key(float z) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) {
   return __uint_as_float(k >> 31 ? k & 0x7FFFFFFFu : ~k);
-}
-
-// 2^y for y <= 0 in 64 bits, times 2^shift: y = n + f with |f| <= 1/2, 2^f by the series of
-// exp(f ln 2) up to the 11th power (the next term is below 2^-47).
-__device__ __forceinline__ double exp2_scaled(double y, int shift) {
-  constexpr double MAGIC = 6755399441055744.0;  // 1.5 x 2^52: adding it rounds to a whole number
-  y = fmax(y, -1000.0);
-  const double t = y + MAGIC;
-  const int n = (int)(uint32_t)__double_as_longlong(t);
-  const double f = y - (t - MAGIC);
-  constexpr double L = 0.693147180559945309417232;
-  constexpr double c2 = L * L / 2, c3 = c2 * L / 3, c4 = c3 * L / 4, c5 = c4 * L / 5, c6 = c5 * L / 6,
-                   c7 = c6 * L / 7, c8 = c7 * L / 8, c9 = c8 * L / 9, c10 = c9 * L / 10,
-                   c11 = c10 * L / 11;
-  double p = fma(f, c11, c10);
-  p = fma(f, p, c9);
-  p = fma(f, p, c8);
-  p = fma(f, p, c7);
-  p = fma(f, p, c6);
-  p = fma(f, p, c5);
-  p = fma(f, p, c4);
-  p = fma(f, p, c3);
-  p = fma(f, p, c2);
-  p = fma(f, p, L);
-  p = fma(f, p, 1.0);
-  return __builtin_ldexp(p, n + shift);
 }
 
 // The weight of a logit, in units of 2^-shift of the largest one's: with y = (z - m) 32 log2(e) / T =

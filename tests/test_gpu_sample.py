@@ -187,6 +187,37 @@ def test_rows_do_not_depend_on_their_neighbours(eng):
     assert (c == a[at]).all() and (lc == la[at]).all()
 
 
+@pytest.mark.parametrize("V", [70, 3000])
+def test_more_rows_than_the_scratch_holds(eng, V):
+    """The workspace holds the scans of 1024 rows here: a call of more comes in several."""
+    z, rng = logits(2300, V, V)
+    rows = rows_of(z, torch.bfloat16)
+    u = rng.random(2300, np.float32)
+    lim = LIMITS["all"](rng, 2300)
+    a, la = draw(eng, rows, u, **lim)
+    for at in (slice(0, 9), slice(1020, 1030), slice(2290, 2300)):
+        b, lb = draw(eng, rows[at], u[at], **{k: v[at] for k, v in lim.items()})
+        assert (a[at] == b).all() and (la[at] == lb).all()
+    pick = np.r_[0:40, 1000:1060, 2040:2060, 2280:2300]
+    z = rows.double().cpu().numpy()
+    for r in pick:
+        assert a[r] == sample_ref(z[r], u[r], **{k: v[r] for k, v in lim.items()})[0]
+
+
+@pytest.mark.parametrize("kind", ["alike", "spread"])
+def test_largest_vocabulary(eng, kind):
+    """The sums of weights at their largest (2^62 units), rows of 2 MiB."""
+    n, V = 6, 524288
+    z, rng = logits(n, V, 31)
+    if kind == "alike":
+        z[:] = -3.25
+    lim = dict(top_k=np.array([0, 0, 300000, 0, 5000, 60]), top_p=np.array([1, 0.9, 0.5, 1, 1, 0.99]),
+               min_p=np.array([0, 0, 0, 1e-3, 0, 0]))
+    rows = rows_of(z, torch.float32)
+    check(eng, rows, rng.random(n, np.float32), **lim)
+    check(eng, rows, rng.random(n, np.float32))
+
+
 def test_captured_replays_and_another_stream(eng):
     n, V = 50, 6001
     z, rng = logits(n, V, 9)
