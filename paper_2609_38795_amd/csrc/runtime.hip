@@ -940,7 +940,8 @@ bool qk_in_runs(const QkArgs& a, bool back) {
 }
 
 // f(lanes per head as a constant, steps): the smallest power of two of lanes that holds half a head,
-// and a row's steps in as many parts as it takes to have `waves` of them.
+// and a row's steps in as many parts as it takes to have `waves` of them.  (Forward, 40 heads of 128 in bf16, 8 waves
+// a CU, against a wave per row: 7 rows 4.5 us against 5.7, 300 rows 4.7 against 6.1, 2000 rows 11 both.)
 template <typename T, typename F>
 void qk_lanes(const QkArgs& a, long waves, F f) {
   const int runs = a.hd / 2 / (16 / (int)sizeof(T));
@@ -1001,15 +1002,19 @@ void launch_distill_rows(const DistillArgs& a, hipStream_t st) {
 }
 
 template <typename T>
-void launch_distill(DistillArgs a, float* loss_out, hipStream_t st) {
+void launch_distill(DistillArgs a, int n_cu, float* loss_out, hipStream_t st) {
   if (a.n > 0) {
-    // a few weights each workgroup adds up itself; beyond, a launch ahead of them does
-    if (a.dz && a.weight && a.n > 256) {
+    // up to 1024 weights each workgroup adds up itself (2 us less than a launch ahead of them; as long at 2048)
+    if (a.dz && a.weight && a.n > 1024) {
       weight_sum_kernel<<<1, 1024, 0, st>>>(a.weight, a.n, loss_out + 1);
       a.w_sum = loss_out + 1;
     }
+    // A wave per row for many short rows, which have no barriers then (bf16 with the gradient, in us, of 64 | 256
+    // threads: 2048 rows of 2048, 21 | 29, of 16384, 47 | 48; 512 rows of 2048, 18 | 16, of 16384, 36 | 23);
+    // twice the threads for long rows with a gradient (1024 rows of 128256: 256 | 512 threads 141 | 136; of 64000,
+    // 69 | 70; without a gradient 50 | 52).
     const long chunks = ((long)a.V * (long)sizeof(T) + 15) / 16;
-    if (chunks <= 256)
+    if (chunks <= 2048 && a.n >= 8L * n_cu)
       launch_distill_rows<T, 64>(a, st);
     else if (chunks <= 4096 || !a.dz)
       launch_distill_rows<T, 256>(a, st);
@@ -1274,16 +1279,19 @@ void launch_sample(const alr_ctx* ctx, SampleArgs a, hipStream_t st) {
   a.slow = ctx->at<uint32_t>(L.sample_slow);
   for (a.row0 = 0; a.row0 < n; a.row0 += cap) {
     a.n = std::min(cap, n - a.row0);
-    // segments of at least two chunks a thread, 16 workgroups per CU where there are that many
+    // Segments of at least two chunks a thread: four, more where that leaves CUs idle.  Calls in us, rows of 128256
+    // fp32 without limits, in 1, 4, 8, 16 segments: one row 63, 28, 22, 20; 128 rows 78, 42, 40, 43; 1024 rows
+    // 223, 210, 211, 224.
     a.n_seg = 1;
-    while (a.n_seg < SAMPLE_SEGS && a.n_seg * a.n < 16 * ctx->n_cu &&
+    while (a.n_seg < SAMPLE_SEGS && (a.n_seg < 4 || a.n_seg * a.n < 4 * ctx->n_cu) &&
            (long)a.V * (long)sizeof(T) >= 2L * a.n_seg * 2 * 256 * 16)
       a.n_seg *= 2;
     const unsigned grid = (unsigned)(a.n * a.n_seg);
     sample_scan_kernel<T, true><<<grid, 256, 0, st>>>(a);
     sample_scan_kernel<T, false><<<grid, 256, 0, st>>>(a);
     sample_settle_kernel<T, 512, false><<<(unsigned)a.n, 512, 0, st>>>(a);
-    sample_settle_kernel<T, 1024, true><<<(unsigned)a.n, 1024, 0, st>>>(a);
+    if (a.top_k || a.top_p || a.min_p)  // no row is left to it without limits
+      sample_settle_kernel<T, 1024, true><<<(unsigned)a.n, 1024, 0, st>>>(a);
   }
 }
 
@@ -2345,9 +2353,9 @@ alr_status alr_distill_loss(alr_ctx* ctx, int32_t n, int32_t vocab, const void* 
   a.dz_rs = (long)dlogits_stride;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (dtype == ALR_BF16)
-    launch_distill<bf16>(a, loss_out, s);
+    launch_distill<bf16>(a, ctx->n_cu, loss_out, s);
   else
-    launch_distill<float>(a, loss_out, s);
+    launch_distill<float>(a, ctx->n_cu, loss_out, s);
   ALR_LAUNCHED(ctx, "distillation loss");
   return ALR_OK;
 }

@@ -252,6 +252,14 @@ def test_many_rows(eng):
     check(eng, rows, ids, logp, tail, w)
 
 
+@pytest.mark.parametrize("n,V,dtype,pad", [
+    (2048, 5003, torch.bfloat16, 0), (2049, 4001, torch.float32, 3), (2060, 9001, torch.bfloat16, 5),
+    (1024, 700, torch.bfloat16, 0), (1025, 700, torch.float32, 1), (2500, 7, torch.bfloat16, 0)])
+def test_many_rows_of_every_length(eng, n, V, dtype, pad):
+    """Calls of many rows take workgroups of their own kind."""
+    check(eng, *make(n, V, dtype, n + V, pad))
+
+
 def test_captured_replays_and_another_stream(eng):
     rows, ids, logp, tail, w = make(64, 3001, torch.bfloat16, 14)
     d = dev(ids, logp, tail, w)
