@@ -357,7 +357,9 @@ __global__ __launch_bounds__(256) void qk_norm_rope_back_kernel(QkArgs a, QkStep
             d[1][k] = rope_b(lo[k], hi[k], cs[k], -sn[k]);
             ss = fmaf(xv[0][k], xv[0][k], fmaf(xv[1][k], xv[1][k], ss));
           }
-          const float inv = 1.0f / sqrtf(head_sum<LPH>(ss) / (float)a.hd + a.eps);
+          // lanes past the last head hold zeros, whose factor would be infinite without eps, and 0 * inf nan
+          const float root = sqrtf(head_sum<LPH>(ss) / (float)a.hd + a.eps);
+          const float inv = h < heads ? 1.0f / root : 0.f;
           float dot = 0.f;
 #pragma unroll
           for (int t = 0; t < 2; ++t)
