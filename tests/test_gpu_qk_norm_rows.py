@@ -51,3 +51,27 @@ def test_no_eps_and_head_counts_that_leave_lanes_idle(n, H, G, hd, dtype, offset
     """A lane without a head has x = 0, whose 1 / sqrt(mean + 0) is infinite."""
     monkeypatch.setattr(op_util, "EPS", 0.0)
     check(n, H, G, hd, dtype, offset, False, 17 * n + H + hd)
+
+
+@pytest.mark.parametrize("n,H,G,hd,dtype,offset,mrope", [
+    (8195, 2, 1, 64, "f32", 0, True), (12289, 4, 1, 128, "bf16", 0, True), (8195, 2, 1, 64, "f32", 1, True),
+    (12289, 4, 1, 128, "bf16", 3, False), (4097, 3, 2, 36, "bf16", 0, True)])
+def test_more_rows_than_the_grid_has_waves(n, H, G, hd, dtype, offset, mrope):
+    """A wave takes a second and a third row: its sums of the gains' gradients go on, its factors are read anew."""
+    check(n, H, G, hd, dtype, offset, mrope, n + hd + offset)
+
+
+def test_a_lost_term_would_show():
+    """The bound on the gains' sums is narrower than one row of one head in at least some columns."""
+    n, H, hd = 12289, 5, 128
+    rng = np.random.default_rng(1)
+    x, dy = rng.standard_normal((2, 64, H, hd))
+    pos = rng.integers(0, 4097, (64, 3))
+    _, _, size = qk_back_ref(x, np.ones(hd), pos, (0, 0, 0), dy)
+    d = np.abs(dy)
+    d = np.tile(d[..., :hd // 2] + d[..., hd // 2:], 2)
+    r = 1 / np.sqrt(np.mean(x * x, 2, keepdims=True) + op_util.EPS)
+    tol = (26 + (-(-n // 4096) + 1) * H + 32) * H_ * np.sum(d * np.abs(x * r), (0, 1)) * n / 64
+    one = [np.abs(qk_back_ref(x[i:i + 1, :1], np.ones(hd), pos[i:i + 1], (0, 0, 0), dy[i:i + 1, :1])[1])
+           for i in range(64)]
+    assert all((t > tol).any() for t in one) and (size > 0).all()
