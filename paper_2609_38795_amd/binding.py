@@ -215,7 +215,7 @@ def decode_plan(shape, max_pos, n_cu: int, seq_len: Sequence[int], anchor_seq, a
 class Engine:
     """One library context: weights repacked into a caller-owned workspace.
 
-    ``weights`` is the generator's dict (numpy float32 or uint16 bf16 bits);
+    ``weights`` is the generator's dict (numpy float32, or uint16 bf16 bits for a bf16 context);
     they are uploaded, repacked by the library and released again.  Layers with
     ``q_norm`` and ``k_norm`` gains [head_dim] turn the per-head q/k norms on.
     """
@@ -272,7 +272,10 @@ class Engine:
         return ctypes.c_void_p(self.stream.cuda_stream)
 
     def _to_dev(self, a: np.ndarray):
+        """Weights on the device, of the context's dtype: the library copies that many bytes a value."""
         torch = self.torch
+        if (a.dtype == np.uint16) != (self.shape.dtype == "bf16"):
+            raise ValueError(f"weights: dtype {a.dtype} for a context of {self.shape.dtype} (bf16: uint16 bits)")
         if a.dtype == np.uint16:
             return torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).to(self.device)
         return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(self.device)
