@@ -264,8 +264,8 @@ class Engine:
             raise AlrError(st, self.lib.alr_last_error(None).decode())
         self.ctx = ctx
         if any("q_norm" in ld or "k_norm" in ld for ld in weights["layers"]):
-            self.set_qk_norm([ld["q_norm"] for ld in weights["layers"]],
-                             [ld["k_norm"] for ld in weights["layers"]])
+            self.set_qk_norm([ld.get("q_norm") for ld in weights["layers"]],
+                             [ld.get("k_norm") for ld in weights["layers"]])
         del dev_w, keep
 
     def _sp(self):
@@ -653,7 +653,8 @@ class Engine:
             st = self.lib.alr_set_qk_norm(self.ctx, None, None, self._sp())
         else:
             hd, nl = self.shape.head_dim, self.shape.n_layers
-            if any(len(gs) != nl or any(g.shape != (hd,) for g in gs) for gs in (q_gain, k_gain)):
+            if any(gs is None or len(gs) != nl or any(g is None or g.shape != (hd,) for g in gs)
+                   for gs in (q_gain, k_gain)):
                 raise ValueError(f"q/k norm gains: {nl} layers of {hd} values each")
             dev = [[self._to_dev(g) for g in gs] for gs in (q_gain, k_gain)]
             arr = [(ctypes.c_void_p * max(1, nl))(*[t.data_ptr() for t in ts]) for ts in dev]

@@ -243,3 +243,14 @@ def test_the_whole_chain():
                  (1 + (x * r).abs())).all())
     assert H == 8 and bool((dg.double() - (x * r).square().sum((0, 1))).abs().max() <= 2.0 ** -6 * n * B * 4 * 2)
     eng.close()
+
+
+def test_weights_with_one_of_the_two_norms_are_refused():
+    inp = _inputs("f32", 64, 8, 2, 13)
+    del inp.weights["layers"][1]["k_norm"]
+    with pytest.raises(ValueError, match="gains"):
+        make_engine(inp)
+    for ld in inp.weights["layers"]:
+        ld.pop("k_norm", None)
+    with pytest.raises(ValueError, match="gains"):
+        make_engine(inp)

@@ -64,3 +64,14 @@ def test_gains_of_the_contexts_type_are_taken(dtype, kind):
     eng = context(dtype)
     eng.set_qk_norm(gains(eng, kind), gains(eng, kind))
     assert len(eng.lib.calls) == 1
+
+
+@pytest.mark.parametrize("case", ["no k", "no q", "one layer's missing", "fewer layers", "another length"])
+def test_incomplete_gains_are_refused(case):
+    eng = context("f32")
+    g = gains(eng, np.float32)
+    q, k = {"no k": (g, None), "no q": (None, g), "one layer's missing": (g, [g[0], None]),
+            "fewer layers": (g[:1], g), "another length": (g, [g[0], g[1][:-1]])}[case]
+    with pytest.raises(ValueError, match="gains"):
+        eng.set_qk_norm(q, k)
+    assert not eng.lib.calls
