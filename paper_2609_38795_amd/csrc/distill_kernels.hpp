@@ -101,11 +101,11 @@ __global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
   __shared__ TailSum red[NW];
   __shared__ double red64[NW];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float inv_w = 0.f;
+  double inv_w = 0.0;  // 64 bits: 1 / W may lie outside fp32 where a weight's share of W does not
   if constexpr (GRAD) {
     const double W = a.w_sum ? (double)a.w_sum[0] : weight_sum(a.weight, a.n, red64);
-    inv_w = W != 0.0 ? (float)((double)a.scale / W) : 0.f;
-    if (a.up) inv_w *= a.up[0];
+    inv_w = W != 0.0 ? (double)a.scale / W : 0.0;
+    if (a.up) inv_w *= (double)a.up[0];
   }
   for (long r = blockIdx.x; r < a.n; r += gridDim.x) {
     RowChunks<T> row(static_cast<const T*>(a.z) + r * a.z_rs, a.V);
@@ -210,7 +210,7 @@ __global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
     const float mass = tau + lane_value(group_sum<8>(lane_pi), 0);
     if (threadIdx.x == 0) a.row_loss[r] = loss;
     if constexpr (GRAD) {
-      const float cw = inv_w * w;
+      const float cw = (float)(inv_w * (double)w);
       const float ref_t = t.m == -INFINITY ? 0.f : t.m;
       // no tail at all: every value outside the list is -inf and gets 0
       const float bt = t.s == 0.f ? 0.f : cw * (mass * expf(lq_tail) - tau) / t.s;
