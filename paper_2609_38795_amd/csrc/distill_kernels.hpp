@@ -28,7 +28,7 @@ struct DistillArgs {
   float scale;
   long n;
   int V;
-  const float* w_sum;    // sum of the weights, or null: each workgroup forms it
+  const float* w_sum;    // sum of the weights as the two halves of a double, or null: each workgroup forms it
   float* row_loss;       // [n]
   void* dz;              // rows of V, or unused
   long dz_rs;
@@ -103,7 +103,8 @@ __global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   double inv_w = 0.0;  // 64 bits: 1 / W may lie outside fp32 where a weight's share of W does not
   if constexpr (GRAD) {
-    const double W = a.w_sum ? (double)a.w_sum[0] : weight_sum(a.weight, a.n, red64);
+    const double W = a.w_sum ? __hiloint2double(__float_as_int(a.w_sum[1]), __float_as_int(a.w_sum[0]))
+                             : weight_sum(a.weight, a.n, red64);
     inv_w = W != 0.0 ? (double)a.scale / W : 0.0;
     if (a.up) inv_w *= (double)a.up[0];
   }
@@ -238,12 +239,16 @@ __global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
   }
 }
 
-// out[0] = sum of the weights, ahead of the gradients of many rows.
+// out[0], out[1] = low and high half of the weights' sum, ahead of the gradients of many rows: the two floats
+// that the loss and W are written to afterwards (aligned to 4 bytes only).
 __global__ __launch_bounds__(1024) void weight_sum_kernel(const float* __restrict__ w, long n,
                                                           float* __restrict__ out) {
   __shared__ double red[16];
   const double W = weight_sum(w, n, red);
-  if (threadIdx.x == 0) out[0] = (float)W;
+  if (threadIdx.x == 0) {
+    out[0] = __int_as_float(__double2loint(W));
+    out[1] = __int_as_float(__double2hiint(W));
+  }
 }
 
 }  // namespace alr

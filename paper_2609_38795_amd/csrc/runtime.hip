@@ -1006,8 +1006,8 @@ void launch_distill(DistillArgs a, int n_cu, float* loss_out, hipStream_t st) {
   if (a.n > 0) {
     // up to 1024 weights each workgroup adds up itself (2 us less than a launch ahead of them; as long at 2048)
     if (a.dz && a.weight && a.n > 1024) {
-      weight_sum_kernel<<<1, 1024, 0, st>>>(a.weight, a.n, loss_out + 1);
-      a.w_sum = loss_out + 1;
+      weight_sum_kernel<<<1, 1024, 0, st>>>(a.weight, a.n, loss_out);
+      a.w_sum = loss_out;
     }
     // A wave per row for many short rows, which have no barriers then (bf16 with the gradient, in us, of 64 | 256
     // threads: 2048 rows of 2048, 21 | 29, of 16384, 47 | 48; 512 rows of 2048, 18 | 16, of 16384, 36 | 23);
