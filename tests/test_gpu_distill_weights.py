@@ -1,9 +1,12 @@
 """Weights at the ends of fp32's range in the distillation loss: the gradient holds only their shares of the sum, which
 are ordinary numbers.  Tolerances as in test_gpu_distill."""
+import math
+
 import numpy as np
 import pytest
 
-from test_gpu_distill import check, dev, eng, make  # noqa: F401
+from op_util import distill_ref
+from test_gpu_distill import H, check, dev, eng, make  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -21,13 +24,33 @@ def test_weights_whose_sum_is_below_the_normal_numbers(eng, n):  # noqa: F811
 
 
 def test_weights_whose_sum_is_beyond_fp32(eng):  # noqa: F811
-    """W is returned as inf where it is, but the loss and the gradient are those of the sum in 64 bits, at any number of rows."""
+    """W is returned as inf where it is, but the loss and the gradient are those of the sum in 64 bits."""
     for n in (8, 1500):
         rows, ids, logp, tail, w = make(n, 90, torch.float32, 22)
-        with np.errstate(over="ignore"):
-            got = check(eng, rows, ids, logp, tail, (w * np.float32(3e38)).astype(np.float32))
+        w = (w * np.float32(3e38)).astype(np.float32)
+        z = rows.double().cpu().numpy()
+        loss, W, row, grad = distill_ref(z, ids, logp, tail, w, 1.013441, 0.75)
+        got = eng.distill_loss(rows, *dev(ids, logp, tail, w), scale=1.013441,
+                               grad_out=torch.tensor([0.75], device="cuda"))
+        torch.cuda.synchronize()
         # 0.52 * 3e38 = 1.6e38 for the eight rows (their first three have weight 0), 181 * 3e38 for the others
-        assert np.isinf(float(got[0][1])) == (n > 8) and bool((got[2] != 0).any())
+        assert np.isinf(float(got[0][1])) == (n > 8)
+        E, size = (math.ceil(90 / 64) + 64) * H, np.abs(z - z.max(1)[:, None]).max(1) + math.log(90) + 1
+        tol = 2 * E * 1.1 + 4 * H * (size + np.abs(row))
+        assert abs(float(got[0][0]) - loss) <= 1.013441 * tol.max() + 2 * H * abs(loss)
+        # the sizes of a gradient's terms, in 64 bits: a share of W is no fp32 quotient here
+        q = np.exp(z - z.max(1)[:, None])
+        outside = np.ones_like(q)
+        np.put_along_axis(outside, ids, 0, 1)
+        tails = q * outside / (q * outside).sum(1, keepdims=True)
+        q /= q.sum(1, keepdims=True)
+        pi = np.exp(logp.astype(np.float64))
+        terms = (pi.sum(1) + tail)[:, None] * q + tail[:, None] * tails
+        np.put_along_axis(terms, ids, np.take_along_axis(terms, ids, 1) + pi, 1)
+        terms *= 0.75 * 1.013441 * (w.astype(np.float64) / W)[:, None]
+        err = np.abs(got[2].double().cpu().numpy() - grad)
+        assert (err <= (2 * E + 8 * H + 6 * H * size[:, None]) * terms + H * np.abs(grad) + 1e-37).all()
+        assert bool((got[2] != 0).any())
 
 
 @pytest.mark.parametrize("V", [90, 700])
