@@ -412,6 +412,9 @@ alr_status alr_rollout_sampled(alr_ctx* ctx, int32_t n_anchor, const int32_t* an
                                int32_t* top_ids_out, float* top_logp_out, float* tail_out,
                                float* logprobs_out, float* feats_out, alr_stream stream);
 
+/* Largest vocabulary of alr_distill_loss: places in a row are counted in 32 bits. */
+#define ALR_DISTILL_MAX_VOCAB 2147483632
+
 /* The distillation loss on top-8 + tail labels, and its gradient (Sec. 3.1, Eq. 1;
  * App. A, the loss row of the training table).  Row r holds a drafter's logits
  * z; its label is one slot of alr_rollout_topk, alr_corpus_labels or
@@ -423,7 +426,7 @@ alr_status alr_rollout_sampled(alr_ctx* ctx, int32_t n_anchor, const int32_t* an
  * times grad_out, by z_v is grad_out scale weight_r / W times
  *   P q_v - sum_{j: id_j = v} pi_j                     for v in S
  *   P q_v - tail q_v / (sum of q outside S)            otherwise.
- *   n, vocab, logits, dtype, row_stride  as in alr_sample (any vocab >= 1).
+ *   n, vocab, logits, dtype, row_stride  as in alr_sample (vocab 1 .. ALR_DISTILL_MAX_VOCAB).
  *   top_ids, top_logp  DEVICE [n, ALR_TOPK]; an id outside [0, vocab) (-1 pads a
  *               label, a cut vocabulary may lack a token) is passed over with its
  *               probability.  An id listed twice adds up.

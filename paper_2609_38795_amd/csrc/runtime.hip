@@ -2324,6 +2324,8 @@ alr_status alr_distill_loss(alr_ctx* ctx, int32_t n, int32_t vocab, const void* 
   if (!ctx) return ALR_E_INVALID_ARG;
   const alr_status st = check_logits(ctx, n, vocab, logits, dtype, row_stride);
   if (st != ALR_OK) return st;
+  if (vocab > ALR_DISTILL_MAX_VOCAB)
+    return fail(ctx, ALR_E_UNSUPPORTED, "vocab %d > %d", vocab, ALR_DISTILL_MAX_VOCAB);
   if (!loss_out) return fail(ctx, ALR_E_INVALID_ARG, "loss_out is NULL");
   if (n > 0 && (!top_ids || !top_logp || !tail || !row_loss_out))
     return fail(ctx, ALR_E_INVALID_ARG,
