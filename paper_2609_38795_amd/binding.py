@@ -579,7 +579,6 @@ class Engine:
 
     def _heads(self, name, t, n):
         """(heads, address, row stride) of rows of heads, or of None."""
-        torch = self.torch
         if t is None:
             return 0, None, 0
         hd = self.shape.head_dim
@@ -641,7 +640,6 @@ class Engine:
         return self._tensor("positions", positions, (n, 3), (self.torch.int32,))
 
     def _gain(self, name, g, heads):
-        torch = self.torch
         if heads == 0:
             return None
         return self._tensor(name, g, (self.shape.head_dim,), self._own_type)

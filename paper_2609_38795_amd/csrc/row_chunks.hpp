@@ -63,7 +63,6 @@ struct RowChunks {
     }
     return w;
   }
-  __device__ __forceinline__ float at(int e) const { return Elt<T>::ld(p + e); }
 };
 
 template <typename T>

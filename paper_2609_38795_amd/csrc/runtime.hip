@@ -960,7 +960,7 @@ void qk_lanes(const QkArgs& a, long waves, F f) {
   else if (runs <= 4) go(std::integral_constant<int, 4>{});
   else if (runs <= 8) go(std::integral_constant<int, 8>{});
   else if (runs <= 16) go(std::integral_constant<int, 16>{});
-  else go(std::integral_constant<int, 32>{});
+  else if constexpr (sizeof(T) == 4) go(std::integral_constant<int, 32>{});  // bf16: 16 runs at most
 }
 
 template <typename T>
@@ -997,7 +997,7 @@ void launch_distill_rows(const DistillArgs& a, hipStream_t st) {
   const unsigned grid = (unsigned)std::min<long>(a.n, 1 << 20);
   if (a.dz)
     distill_rows_kernel<T, THREADS, true><<<grid, THREADS, 0, st>>>(a);
-  else
+  else if constexpr (THREADS <= 256)  // 512 threads: with a gradient only
     distill_rows_kernel<T, THREADS, false><<<grid, THREADS, 0, st>>>(a);
 }
 

@@ -249,11 +249,11 @@ struct Aim {
 };
 
 // Finds the aim's bin; above_c and above_m come in as what lies before the level's bins and go out as
-// what lies before the bin.  Returns -1 where the bins do not reach it.  mass_of(total weight of
-// the bins) may still set the aim (a share of a whole that only the bins know).
+// what lies before the bin.  Returns -1 where the bins do not reach it.  total_of is told the
+// total weight of the bins.
 template <int THREADS, typename S, typename F>
-__device__ __forceinline__ int find_bin(S& sh, int level, Aim& aim, uint32_t& above_c,
-                                        u64& above_m, F mass_of) {
+__device__ __forceinline__ int find_bin(S& sh, int level, Aim aim, uint32_t& above_c,
+                                        u64& above_m, F total_of) {
   constexpr int NW = THREADS / 64, PER = SAMPLE_BINS / THREADS;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b0 = threadIdx.x * PER;
   uint32_t c = 0;
@@ -280,7 +280,7 @@ __device__ __forceinline__ int find_bin(S& sh, int level, Aim& aim, uint32_t& ab
     }
     all += sh.scan_m[i];
   }
-  mass_of(all);
+  total_of(all);
   uint32_t c_before = above_c + c_upto - c;
   u64 m_before = above_m + m_upto - m;
   u64 at = aim.by_mass ? m_before : c_before;
@@ -695,8 +695,8 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
       f(v, row.first(c));
     });
   };
-  using light = std::integral_constant<int, 4>;
-  using heavy = std::integral_constant<int, 4>;  // passes that weigh every logit
+  using four = std::integral_constant<int, 4>;  // loads of a thread under way; `one` needs fewer registers
+  using one = std::integral_constant<int, 1>;
   auto each = [&](auto u_, auto f) {
     chunks(u_, [&](const float(&v)[EPC], int e0) {
 #pragma unroll
@@ -744,7 +744,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
   auto bin_row = [&]() {
     clear_bins<THREADS>(sh, 1);
     if (by_p)
-      each(heavy{}, [&](float z, int) {
+      each(four{}, [&](float z, int) {
         if (real(z)) {
           const int q = bin0(z);
           if (by_k) atomicAdd(&sh.cnt[1][q], 1u);
@@ -752,7 +752,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
         }
       });
     else
-      each(light{}, [&](float z, int) {
+      each(four{}, [&](float z, int) {
         if (real(z)) atomicAdd(&sh.cnt[1][bin0(z)], 1u);
       });
     __syncthreads();
@@ -813,7 +813,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
       });
     };
     auto visit_row = [&](auto f) {
-      each(std::integral_constant<int, 1>{}, [&](float z, int e) {
+      each(one{}, [&](float z, int e) {
         if (real(z) && z >= from && z <= upto) f(up ? (uint32_t)e : order_key(z), z);
       });
     };
@@ -828,7 +828,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_settle_kernel(SampleArgs a)
       aside.mine = 0;
       lo = 0xFFFFFFFFu;
       hi = 0;
-      chunks(light{}, [&](const float(&v)[EPC], int e0) {
+      chunks(four{}, [&](const float(&v)[EPC], int e0) {
         uint32_t in = 0;
 #pragma unroll
         for (int q = 0; q < EPC; ++q) {
