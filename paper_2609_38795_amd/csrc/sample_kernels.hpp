@@ -389,12 +389,12 @@ struct Cut {
 };
 constexpr u64 ALL_TIES = ~0ull;
 
-// The lowest float whose weight is at least min_p: near m + T ln p, then step by step.
+// The lowest float whose weight is at least min_p: near m + T ln p (or the lowest of all), then step by step.
 __device__ __forceinline__ float min_p_cut(const Weigher& wt, float m, float mp) {
   const double want = fmin((double)mp, 1.0);
   auto keeps = [&](float z) { return exp2(wt.log2_of(z)) >= want; };
   const uint32_t top = order_key(m);
-  uint32_t key = min(order_key((float)fmax(wt.m + 32 * log2(want) / wt.c, -3.4e38)), top);
+  uint32_t key = min(order_key((float)fmax(wt.m + 32 * log2(want) / wt.c, -(double)3.402823466e38f)), top);
   for (int i = 0; i < 64 && key < top && !keeps(key_value(key)); ++i) ++key;
   for (int i = 0; i < 64 && key > 0x00800000u && keeps(key_value(key - 1)); ++i) --key;
   return key_value(key);
