@@ -393,6 +393,7 @@ constexpr u64 ALL_TIES = ~0ull;
 __device__ __forceinline__ float min_p_cut(const Weigher& wt, float m, float mp) {
   const double want = fmin((double)mp, 1.0);
   auto keeps = [&](float z) { return exp2(wt.log2_of(z)) >= want; };
+  if (want == 1.0) return m;  // the others' weights are below 1, though they may round to it
   const uint32_t top = order_key(m);
   uint32_t key = min(order_key((float)fmax(wt.m + 32 * log2(want) / wt.c, -(double)3.402823466e38f)), top);
   for (int i = 0; i < 64 && key < top && !keeps(key_value(key)); ++i) ++key;
