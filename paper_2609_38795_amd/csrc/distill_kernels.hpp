@@ -88,10 +88,10 @@ __device__ __forceinline__ float lane_value(float v, int lane) {
 }
 
 // One workgroup per row, which reads it for the sums and, with a gradient, again, mostly from the last-level
-// cache (keeping part of it in LDS or registers in between measured no faster).  The running maximum of the sums
+// cache (keeping part of a row of 128256 in LDS or registers in between measured no faster).  The running maximum of the sums
 // costs one exponential a chunk; they are formed while later loads are under way.  What bounds it is HBM.  Call
-// times: the loss of 768 fp32 rows of 152064, 79-82 us (5.7 TB/s or more); with the gradient in bf16, 4096 rows of 32000, 140
-// us and 2048 rows of 128256, 254 us (3.7 and 4.1 TB/s of one read and one write; the second read is the rest).
+// times: the loss of 768 fp32 rows of 152064, 77 us (6.1 TB/s); with the gradient in bf16, 4096 rows of 32000, 141
+// us and 2048 rows of 128256, 256 us (3.7 and 4.1 TB/s of one read and one write; the second read is the rest).
 //
 // Chunks that hold listed tokens (eight at most) are left out of both passes: lane j of every wave loads entry
 // j's chunk at the start, and the first wave's lanes take them at the end of each pass, all at once.

@@ -168,7 +168,8 @@ __device__ __forceinline__ float head_sum(float v) {
 // one run of VEC values of the low half and the one that is turned with it, 64 / LPH heads of a row at a
 // time.  The factors of the row's position are read once per wave, and the loads of U such steps go out before
 // the first use.  What bounds it is HBM: 32768 rows of 40 bf16 heads of 128 take 125 us (5.4 TB/s, a large
-// copy's 5.2); a wave per head, with a pair per lane, took 516.  Seven rows take the kernel 4 us.
+// copy's 5.2); a wave per head, with a pair per lane, took 516.  Seven rows take the kernel 4 us.  Registers leave
+// three waves a SIMD in bf16 (129, four waves from 128 on), four in fp32.
 template <typename T, int LPH>
 struct QkLane {
   static constexpr int VEC = 16 / (int)sizeof(T), HPW = 64 / LPH;
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a, QkSteps st)
 // Backward: the grid's waves walk the (row, part) units; a lane keeps the gain gradients of its runs in
 // registers until the end, then the heads of a wave meet by shuffles and the waves in LDS.  8192 rows of 32
 // bf16 heads of 128: 46 us (4.4 TB/s of two reads and a write), and 5 for the gains' sums; 2047 rows of 20 fp32
-// heads of 64: 10 and 3.
+// heads of 64: 10 and 3.  186 registers in bf16 leave two waves a SIMD, half of those the grid brings; 129 in fp32, three.
 template <typename T, int LPH>
 __global__ __launch_bounds__(256) void qk_norm_rope_back_kernel(QkArgs a, QkSteps st) {
   using L = QkLane<T, LPH>;

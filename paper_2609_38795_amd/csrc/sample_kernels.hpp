@@ -12,11 +12,12 @@
 // first takes the maximum and, from the maxima of a thousand parts, a line above which a few thousand
 // logits lie; the second sets those aside, and adds up the row's weight where top_p is of the whole
 // row.  A third settles every row whose limits fall within its list, a fourth the others, from
-// histograms of the row.  1024 rows of 128256 fp32 with all limits, in microseconds: 81 (6.5 TB/s, part of it from
-// the last-level cache), 137 (the rows whose weight is summed: 64-bit arithmetic), 62, 115: 398 for the
+// histograms of the row.  1024 rows of 128256 fp32 with all limits, in microseconds: 82 (6.4 TB/s, part of it from
+// the last-level cache), 135 (80 to read the rows, 20 to set the lists aside, 35 for the weights of the 192 rows
+// that need them, 13 if their work were spread evenly), 63, 116: 396 for the
 // call, where a first kernel that did it all in one launch, a row per workgroup and a pass of the row per
 // narrowing, took 989, and one with the list and all else in one launch 505.  128 rows without limits:
-// 13 + 21 + 9, 37 for the call.
+// 12 + 18 + 8, 37 for the call.
 //
 // Weights are whole numbers of 2^-shift (shift >= 43), from 64-bit exponentials, so every sum is exact
 // and does not depend on the order in which it is formed: what a row gives depends on its own values
@@ -137,8 +138,9 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 // k + f, |f| <= 1/2, the weight is 2^(k / 32) times a polynomial of 2^(f / 32).  2^((k mod 32) / 32) comes from a
 // table, the rest of k is added to its exponent, and adding 2^52 rounds to whole units.  The polynomial is
 // the series of exp up to the 5th power with that power replaced by the lower ones that differ least
-// from it on [-1/2, 1/2] (Chebyshev): 2^-43 of the weight.  Some 25 instructions of which a wave issues about
-// one a cycle (31 cycles a weight): what bounds every pass that weighs a whole row.
+// from it on [-1/2, 1/2] (Chebyshev): 2^-43 of the weight.  Some 25 instructions, which bound every pass that weighs
+// whole rows: in a scan of 1024 rows of 128256 that sets lists aside, weighing all rows takes 175 us and none 104,
+// 85 cycles of a SIMD for the 64 weights of a wave.
 struct Weigher {
   double m, c, floor;  // the row's largest logit; 32 log2(e) / T; the lowest z - m: weights below are 0
   int shift;
@@ -644,7 +646,7 @@ __global__ __launch_bounds__(256, 4) void sample_scan_kernel(SampleArgs a) {
 
 // Settles a row from what the scans left.  Limits that fall within the list are settled there, and so is the
 // draw; without limits the part of the row that the number falls into is read again.  What bounds it is the
-// chain of picks, each some eight barriers long: 17 us for one row, 62 for 1024.  Rows whose list falls short (a
+// chain of picks, each some eight barriers long: 17 us for one row, 63 for 1024.  Rows whose list falls short (a
 // nucleus of a flat distribution, a k of thousands) are left to the SLOW form, a launch of its own, whose
 // workgroups have a CU to themselves: a histogram of the row, the list becomes that of the bin the limit falls
 // into, and the draw reads the row again.  A row of 128256 takes it 100 us (histogram 36, list 25, draw 29), bound
